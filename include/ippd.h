@@ -60,6 +60,7 @@ typedef enum {
 /* Bits OR-ed into *err_flag by device code. */
 #define IPPD_FLAG_SEGMENT_FULL 1  /* append found seg_len[i] == seg_capacity: token dropped */
 #define IPPD_FLAG_BAD_LAYOUT   2  /* device arrays break a rule below: rows skipped */
+#define IPPD_FLAG_PAGES_EXHAUSTED 4  /* ippd_paged_reserve: fewer free pages than needed, tokens refused */
 
 /*
  * Batch description (a host struct; its array fields are device pointers).
@@ -361,6 +362,141 @@ ippd_status_t ippd_prefill_attention(const ippd_batch_t *batch, int32_t max_prom
 ippd_status_t standard_prefill_attention(const ippd_batch_t *batch, int32_t max_prompt_question_tokens,
                                          const void *q_ctx, const void *q_seg, const ippd_kv_cache_t *kv,
                                          float *out_ctx, float *out_seg, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Paged cache.  The contiguous cache above gives every question seg_capacity
+ * tokens from the start and keeps each context in one piece of the pool.  Here
+ * keys and values live in pages of page_tokens tokens that sequences take as
+ * they grow and give back when they end.
+ *
+ * Sequences are numbered s = 0 .. B + Nt - 1: the contexts of the prompts first,
+ * then the segments of the questions (sequence B + i is question i's).  Token t
+ * of sequence s sits in page block_table[s][t / page_tokens], at offset
+ * t % page_tokens; its slot is page * page_tokens + offset.  A sequence of
+ * seq_len[s] tokens holds the first ceil(seq_len[s] / page_tokens) pages of its
+ * row of the table; what the rest of the row holds is not read.  Virtual
+ * positions are those of the contiguous cache: t in a context, seq_len of the
+ * prompt's context + t in a segment.
+ *
+ * free_pages[0 .. *free_count - 1] is a stack of the pages that no sequence
+ * holds (top at the end); ippd_paged_reserve moves pages between it and the
+ * tables.  A page is held by one sequence at a time.
+ * ------------------------------------------------------------------------ */
+#define IPPD_PAGED_MAX_SEQUENCES (1 << 20)   /* num_prompts + num_questions */
+#define IPPD_PAGED_MAX_ROWS (1 << 26)        /* rows of one reserve or append call */
+
+typedef struct ippd_paged_batch {
+  int32_t num_prompts;       /* B >= 1 */
+  int32_t num_questions;     /* Nt >= 0, total over prompts; Nt * Hkv <= 2^23 */
+  int32_t num_q_heads;       /* Hq, 1..1024 */
+  int32_t num_kv_heads;      /* Hkv >= 1, Hq % Hkv == 0, Hq/Hkv <= 16 */
+  int32_t head_dim;          /* D: 64 or 128 */
+  int32_t dtype;             /* ippd_dtype_t */
+  int32_t page_tokens;       /* 16, 32, 64, 128 or 256 */
+  int32_t num_pages;         /* pages of the pool, >= 1; num_pages * page_tokens < 2^31 */
+  int32_t table_pages;       /* entries of a row of the block table, >= 1; table_pages * page_tokens < 2^31 */
+  int32_t max_questions;     /* host bound on questions per prompt, 1..1024 */
+  double  rope_base;         /* > 0, e.g. 10000 */
+  float   scale;             /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+  const int32_t *q_start;    /* [B+1] question CSR offsets, as in ippd_batch_t */
+  int32_t       *seq_len;    /* [B + Nt] tokens of each sequence; moved by ippd_paged_reserve */
+  int32_t       *block_table;/* [B + Nt][table_pages] */
+  int32_t       *free_pages; /* [num_pages] */
+  int32_t       *free_count; /* [1] */
+  const uint8_t *active;     /* [Nt]  1 = decoding this step */
+  int32_t       *err_flag;   /* [1]   IPPD_FLAG_* bits (never cleared by the library) */
+} ippd_paged_batch_t;
+
+/*
+ * Pages of one layer (device, batch dtype, 16-byte aligned).  Keys are stored
+ * rotated, values in 8-token column blocks:
+ *   k [num_pages][Hkv][page_tokens][D]     v [num_pages][Hkv][page_tokens / 8][D][8]
+ */
+typedef struct ippd_pages {
+  void *k;
+  void *v;
+} ippd_pages_t;
+
+/*
+ * Lengths, block tables and slots of a change of the sequences, once for all
+ * layers.  new_tokens[s] (device [B + Nt]) is sequence s's change:
+ *   > 0   tokens are added: pages come from the stack, seq_len[s] grows.  Their
+ *         rows in this call's slot map are token_start[s] + 0 .. new_tokens[s]-1;
+ *   < 0   the last -new_tokens[s] tokens are taken back (a rejected draft), all
+ *         of them if it holds fewer (a request's end); pages that hold no token
+ *         any more go back to the stack;
+ *   0     nothing.
+ * Pages given back in a call are there for what the call adds.  token_start
+ * (device [B + Nt + 1], non-decreasing, within 0 .. num_rows) says which rows
+ * belong to s; it may hold more rows than s adds tokens, so that a decode step
+ * can keep row i for question i.  Outputs, device:
+ *   slot_map [num_rows]   the slot of each row's token, -1 where a row has none;
+ *   positions [num_rows]  its virtual position, by the lengths after the call, or -1;
+ *   served [B + Nt]       tokens added to (or, negative, taken from) each sequence.
+ * A sequence is served whole or not at all: not if its row of the table is full
+ * (IPPD_FLAG_SEGMENT_FULL), nor if the pages needed by the sequences up to it
+ * outnumber the free ones (IPPD_FLAG_PAGES_EXHAUSTED).
+ * Pages are taken and given back in the order of sequences and, within one, of
+ * its tokens: the k-th page taken is the k-th from the top of the stack, and a
+ * call that takes back what the call before it added restores the stack.
+ * Lengths, offsets or counts that break the rules set IPPD_FLAG_BAD_LAYOUT and
+ * the whole call moves nothing (served 0, slots -1).
+ */
+ippd_status_t ippd_paged_reserve(const ippd_paged_batch_t *batch, const int32_t *new_tokens,
+                                 const int32_t *token_start, int32_t num_rows, int32_t *slot_map,
+                                 int32_t *positions, int32_t *served, hipStream_t stream);
+
+/*
+ * Rotate new tokens and write them into the pages of one layer.  For every row
+ * r < num_rows with slot_map[r] >= 0, pos = positions[r]:
+ *   k at slot_map[r] <- R(pos) k[r], v at slot_map[r] <- v[r],
+ *   q_rot[r][h] = R(pos) q[r][h]    if q is not NULL (a prefill rotates its own).
+ * q [num_rows][Hq][D], k, v [num_rows][Hkv][D] (batch dtype); row r of each
+ * starts *_stride elements after row r-1 (at least a row, a multiple of 16
+ * bytes), so views of one joint projection do.  q_rot [num_rows][Hq][D] is
+ * contiguous and overlaps no input.  Rows with slot -1 are not written; a slot
+ * outside the pool sets IPPD_FLAG_BAD_LAYOUT and its row is skipped.  The slots
+ * of a call are distinct; if one occurs twice, which of its rows' values it
+ * keeps is not defined.
+ */
+ippd_status_t ippd_paged_append(const ippd_paged_batch_t *batch, const ippd_pages_t *pages, int32_t num_rows,
+                                const int32_t *slot_map, const int32_t *positions, const void *q, int64_t q_stride,
+                                const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_rot,
+                                hipStream_t stream);
+
+/*
+ * How the attention of a decode step is spread over the chip, from the lengths
+ * and active flags on the device: call it once a step, after
+ * ippd_paged_reserve, and use the plan for every layer.  plan: device, 256-byte
+ * aligned, ippd_paged_plan_bytes(batch) bytes (0: invalid batch), overwritten
+ * whole.  A plan keeps the lengths and flags of its call.  Lengths or offsets
+ * that break the rules set IPPD_FLAG_BAD_LAYOUT and the plan serves no question.
+ */
+size_t ippd_paged_plan_bytes(const ippd_paged_batch_t *batch);
+ippd_status_t ippd_paged_plan(const ippd_paged_batch_t *batch, void *plan, size_t plan_bytes, hipStream_t stream);
+
+/*
+ * IPPD decode-step attention over the paged cache: for every question i that
+ * was active when the plan was made, and query head h,
+ *   out[i][h] = softmax_k( scale * q_rot[i][h] . K_k ) V_k
+ * over the keys of its prompt's context and of its own segment (the step's own
+ * token among them, if it was appended).  A context's pages are read once for
+ * all of its active questions.  q_rot and out [Nt][Hq][D] are of the batch
+ * dtype (the output feeds a projection of that type; sums and softmax
+ * statistics are fp32), lse [Nt][Hq] float32 or NULL.  A question without any
+ * key gets zeros and lse -inf.  Rows of inactive questions are not written, nor
+ * those of a question that a page id outside the pool is met for
+ * (IPPD_FLAG_BAD_LAYOUT).  A buffer that holds no plan of this batch's sizes
+ * sets the same flag and nothing is written.
+ * workspace: device, 256-byte aligned, ippd_paged_workspace_bytes(batch) bytes;
+ * it needs no initialisation and carries nothing between calls; calls that may
+ * run concurrently need separate ones (they may share a plan).
+ * Two kernel launches.
+ */
+size_t ippd_paged_workspace_bytes(const ippd_paged_batch_t *batch);
+ippd_status_t ippd_paged_decode_attention(const ippd_paged_batch_t *batch, const ippd_pages_t *pages,
+                                          const void *plan, size_t plan_bytes, const void *q_rot, void *out,
+                                          float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Static description of a status code. */
 const char *ippd_status_string(ippd_status_t status);

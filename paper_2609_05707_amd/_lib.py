@@ -28,6 +28,9 @@ IPPD_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 IPPD_FLAG_SEGMENT_FULL = 1
 IPPD_FLAG_BAD_LAYOUT = 2
+IPPD_FLAG_PAGES_EXHAUSTED = 4
+IPPD_PAGED_MAX_SEQUENCES = 1 << 20
+IPPD_PAGED_MAX_ROWS = 1 << 26
 
 EXPORTED = [
     "ippd_load_context", "ippd_load_instructions", "ippd_load_segments", "ippd_append_kv",
@@ -36,6 +39,8 @@ EXPORTED = [
     "dense_decode_workspace_bytes", "dense_decode_attention",
     "ippd_decode_step", "standard_decode_step", "ippd_decode_step_noalloc",
     "ippd_prefill_attention", "standard_prefill_attention",
+    "ippd_paged_reserve", "ippd_paged_append", "ippd_paged_plan_bytes", "ippd_paged_plan",
+    "ippd_paged_workspace_bytes", "ippd_paged_decode_attention",
     "ippd_status_string", "ippd_last_hip_error", "ippd_version",
 ]
 
@@ -75,6 +80,36 @@ class IppdBatch(ctypes.Structure):
 class IppdKvCache(ctypes.Structure):
     """Mirror of ippd_kv_cache_t."""
     _fields_ = [("ctx_k", c_void_p), ("ctx_vt", c_void_p), ("seg_k", c_void_p), ("seg_vt", c_void_p)]
+
+
+class IppdPagedBatch(ctypes.Structure):
+    """Mirror of ippd_paged_batch_t."""
+    _fields_ = [
+        ("num_prompts", c_int32),
+        ("num_questions", c_int32),
+        ("num_q_heads", c_int32),
+        ("num_kv_heads", c_int32),
+        ("head_dim", c_int32),
+        ("dtype", c_int32),
+        ("page_tokens", c_int32),
+        ("num_pages", c_int32),
+        ("table_pages", c_int32),
+        ("max_questions", c_int32),
+        ("rope_base", c_double),
+        ("scale", c_float),
+        ("q_start", c_void_p),
+        ("seq_len", c_void_p),
+        ("block_table", c_void_p),
+        ("free_pages", c_void_p),
+        ("free_count", c_void_p),
+        ("active", c_void_p),
+        ("err_flag", c_void_p),
+    ]
+
+
+class IppdPages(ctypes.Structure):
+    """Mirror of ippd_pages_t."""
+    _fields_ = [("k", c_void_p), ("v", c_void_p)]
 
 
 class IppdError(RuntimeError):
@@ -122,6 +157,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         getattr(lib, name).argtypes = [P(IppdBatch), ctypes.c_int32, c_void_p, c_void_p, P(IppdKvCache), c_void_p,
                                        c_void_p, c_void_p]
         getattr(lib, name).restype = st
+    lib.ippd_paged_reserve.argtypes = [P(IppdPagedBatch), c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                       c_void_p]
+    lib.ippd_paged_append.argtypes = [P(IppdPagedBatch), P(IppdPages), c_int32, c_void_p, c_void_p, c_void_p, c_int64,
+                                      c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]
+    lib.ippd_paged_plan.argtypes = [P(IppdPagedBatch), c_void_p, c_size_t, c_void_p]
+    lib.ippd_paged_decode_attention.argtypes = [P(IppdPagedBatch), P(IppdPages), c_void_p, c_size_t, c_void_p, c_void_p,
+                                                c_void_p, c_void_p, c_size_t, c_void_p]
+    for name in ("ippd_paged_reserve", "ippd_paged_append", "ippd_paged_plan", "ippd_paged_decode_attention"):
+        getattr(lib, name).restype = st
+    for name in ("ippd_paged_plan_bytes", "ippd_paged_workspace_bytes"):
+        getattr(lib, name).argtypes = [P(IppdPagedBatch)]
+        getattr(lib, name).restype = c_size_t
     lib.ippd_status_string.argtypes = [c_int]
     lib.ippd_status_string.restype = ctypes.c_char_p
     lib.ippd_last_hip_error.argtypes = []
@@ -223,6 +270,38 @@ def standard_prefill_attention(batch, max_prompt_question_tokens, q_ctx, q_seg, 
     _check("standard_prefill_attention",
            load_library().standard_prefill_attention(ctypes.byref(batch), max_prompt_question_tokens, q_ctx, q_seg,
                                                      ctypes.byref(kv), out_ctx, out_seg, stream))
+
+
+def ippd_paged_reserve(batch, new_tokens, token_start, num_rows, slot_map, positions, served, stream) -> None:
+    _check("ippd_paged_reserve",
+           load_library().ippd_paged_reserve(ctypes.byref(batch), new_tokens, token_start, num_rows, slot_map, positions,
+                                             served, stream))
+
+
+def ippd_paged_append(batch, pages, num_rows, slot_map, positions, q, q_stride, k, k_stride, v, v_stride, q_rot,
+                      stream) -> None:
+    _check("ippd_paged_append",
+           load_library().ippd_paged_append(ctypes.byref(batch), ctypes.byref(pages), num_rows, slot_map, positions, q,
+                                            q_stride, k, k_stride, v, v_stride, q_rot, stream))
+
+
+def ippd_paged_plan_bytes(batch) -> int:
+    return int(load_library().ippd_paged_plan_bytes(ctypes.byref(batch)))
+
+
+def ippd_paged_plan(batch, plan, plan_bytes, stream) -> None:
+    _check("ippd_paged_plan", load_library().ippd_paged_plan(ctypes.byref(batch), plan, plan_bytes, stream))
+
+
+def ippd_paged_workspace_bytes(batch) -> int:
+    return int(load_library().ippd_paged_workspace_bytes(ctypes.byref(batch)))
+
+
+def ippd_paged_decode_attention(batch, pages, plan, plan_bytes, q_rot, out, lse, workspace, workspace_bytes,
+                                stream) -> None:
+    _check("ippd_paged_decode_attention",
+           load_library().ippd_paged_decode_attention(ctypes.byref(batch), ctypes.byref(pages), plan, plan_bytes, q_rot,
+                                                      out, lse, workspace, workspace_bytes, stream))
 
 
 def raw_status(fn: str, *args) -> int:

@@ -1,0 +1,229 @@
+// Rotation of new tokens at their virtual positions (Sec. 4.1) and their write
+// into pages through the slot map.
+//
+// A token's slot is page * page_tokens + offset.  Its key goes to row `offset`
+// of the page's keys, its value to column offset % 8 of the page's 8-token
+// block offset / 8.  Cos and sin come from the fp64-reduced angle
+// (rope_cos_sin) and rotations round as in the contiguous cache's kernels, so
+// both caches hold the same bits.
+//
+// What bounds it is the copy, every byte of q, k and v loaded and stored once;
+// for a decode step's few tokens the latency of one load and one store.
+#include <algorithm>
+
+#include "ippd_device.h"
+#include "paged_internal.h"
+
+namespace ippd {
+
+namespace {
+
+constexpr int kStepRows = 1024;   // up to so many rows a workgroup takes one row, above them eight
+
+template <typename T> struct Vec16 { static constexpr int N = 16 / static_cast<int>(sizeof(T)); typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
+template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8))); };
+
+// Element of the slot's key row, and of column 0 of its value block, for kv head g.
+__device__ __forceinline__ int64_t key_at(const PagedAppendParams& p, int slot, int g) {
+  const int off = slot & ((1 << p.page_shift) - 1);
+  return ((((static_cast<int64_t>(slot >> p.page_shift) * p.Hkv + g) << p.page_shift) + off)) * p.D;
+}
+__device__ __forceinline__ int64_t value_at(const PagedAppendParams& p, int slot, int g) {
+  const int off = slot & ((1 << p.page_shift) - 1) & ~7;
+  return ((((static_cast<int64_t>(slot >> p.page_shift) * p.Hkv + g) << p.page_shift) + off)) * p.D;
+}
+
+// One row a workgroup, one 16-byte vector (of each half, for q and k) per
+// thread and pass: every load goes out before the row's slot is known, the
+// row's D/2 angles are evaluated once, into LDS.
+template <typename T>
+__global__ __launch_bounds__(1024) void append_row_kernel(PagedAppendParams p) {
+  constexpr int VE = Vec16<T>::N;
+  typedef typename Vec16<T>::type vec_t;
+  const int row = blockIdx.x, half = p.D / 2;
+  const int QP = half / VE, VG = p.D / VE;
+  const int nq = p.q ? p.Hq * QP : 0, nk = p.Hkv * QP, items = nq + nk + p.Hkv * VG;
+  __shared__ float2 rot[kMaxHalfDim];
+  const T* __restrict__ q = static_cast<const T*>(p.q) + row * p.q_stride;
+  const T* __restrict__ k = static_cast<const T*>(p.k) + row * p.k_stride;
+  const T* __restrict__ v = static_cast<const T*>(p.v) + row * p.v_stride;
+  const int slot = p.slot_map[row], pos = p.positions[row];
+  const double theta = threadIdx.x < static_cast<unsigned>(half) ? p.inv_freq[threadIdx.x] : 0.0;
+  auto source = [&](int e, int& hoff) {
+    hoff = half;
+    if (e < nq) return q + (e / QP) * p.D + (e % QP) * VE;
+    if (e < nq + nk) return k + ((e - nq) / QP) * p.D + ((e - nq) % QP) * VE;
+    hoff = 0;
+    return v + (e - nq - nk) * VE;
+  };
+  vec_t lo, hi;
+  if (threadIdx.x < static_cast<unsigned>(items)) {
+    int hoff;
+    const T* src = source(threadIdx.x, hoff);
+    lo = *reinterpret_cast<const vec_t*>(src);
+    hi = *reinterpret_cast<const vec_t*>(src + hoff);
+  }
+  if (slot < 0) return;
+  if (slot >= p.slots) {
+    if (threadIdx.x == 0) raise_flag(p.err_flag, kFlagBadLayout);
+    return;
+  }
+  if (threadIdx.x < static_cast<unsigned>(half)) {
+    float c, sn;
+    rope_cos_sin(pos, theta, c, sn);
+    rot[threadIdx.x] = make_float2(c, sn);
+  }
+  __syncthreads();                                   // the slot is the row's: every thread is here
+  for (int e = threadIdx.x; e < items; e += blockDim.x) {
+    if (e >= static_cast<int>(blockDim.x)) {
+      int hoff;
+      const T* src = source(e, hoff);
+      lo = *reinterpret_cast<const vec_t*>(src);
+      hi = *reinterpret_cast<const vec_t*>(src + hoff);
+    }
+    if (e < nq + nk) {
+      const int ee = e < nq ? e : e - nq;
+      const int h = ee / QP, j0 = (ee % QP) * VE;
+      vec_t x, y;
+#pragma unroll
+      for (int u = 0; u < VE; ++u) {
+        const float2 cs = rot[j0 + u];
+        float xr, yr;
+        rope_rotate(to_f32<T>(lo[u]), to_f32<T>(hi[u]), cs.x, cs.y, xr, yr);
+        x[u] = from_f32<T>(xr);
+        y[u] = from_f32<T>(yr);
+      }
+      T* dst = e < nq ? static_cast<T*>(p.q_rot) + (static_cast<int64_t>(row) * p.Hq + h) * p.D + j0
+                      : static_cast<T*>(p.k_pages) + key_at(p, slot, h) + j0;
+      *reinterpret_cast<vec_t*>(dst) = x;
+      *reinterpret_cast<vec_t*>(dst + half) = y;
+    } else {
+      const int ev = e - nq - nk, g = ev / VG, d0 = (ev % VG) * VE;
+      T* dst = static_cast<T*>(p.v_pages) + value_at(p, slot, g) + d0 * 8 + (slot & 7);
+#pragma unroll
+      for (int u = 0; u < VE; ++u) dst[u * 8] = lo[u];
+    }
+  }
+}
+
+// Eight rows a workgroup.  Waves 0 and 1 turn keys, 2 and 3 carry the values,
+// then all turn the queries: lane (row, 8 pairs) evaluates its angles once for
+// all heads.  Values: eight rows in consecutive slots of one 8-token block are
+// transposed in registers into 16-byte pieces (fp32: 32) and written by the
+// workgroup that holds the first of them, so that a fill whose rows do not
+// start on a multiple of eight writes whole blocks too; other rows are written
+// by themselves, element by element.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
+  typedef typename Vec8<T>::type vec_t;
+  constexpr int half = D / 2, P = half / 8, HPW = 64 / (8 * P);   // pieces of 8 pairs a row; heads a wave holds
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r0 = blockIdx.x * 8;
+  // slots of rows r0 - 7 .. r0 + 14: whether a block is whole takes its rows' all
+  __shared__ int near[24];
+  if (threadIdx.x < 22) {
+    const int r = r0 - 7 + static_cast<int>(threadIdx.x);
+    int slot = r >= 0 && r < p.num_rows ? p.slot_map[r] : -1;
+    if (slot >= p.slots) {
+      raise_flag(p.err_flag, kFlagBadLayout);
+      slot = -1;
+    }
+    near[threadIdx.x] = slot;
+  }
+  const int t = lane / P % 8, j0 = (lane % P) * 8, hs = lane / (8 * P);
+  const int row = min(r0 + t, p.num_rows - 1);
+  const int pos = p.positions[row];
+  float cs[8], sn[8];
+  if (wave < 2 || p.q) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) rope_cos_sin(pos, p.inv_freq[j0 + u], cs[u], sn[u]);
+  }
+  __syncthreads();
+  const int slot = r0 + t < p.num_rows ? near[7 + t] : -1;
+  auto turn = [&](const T* src, T* dst) {
+    const vec_t lo = *reinterpret_cast<const vec_t*>(src);
+    const vec_t hi = *reinterpret_cast<const vec_t*>(src + half);
+    vec_t x, y;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      float xr, yr;
+      rope_rotate(to_f32<T>(lo[u]), to_f32<T>(hi[u]), cs[u], sn[u], xr, yr);
+      x[u] = from_f32<T>(xr);
+      y[u] = from_f32<T>(yr);
+    }
+    *reinterpret_cast<vec_t*>(dst) = x;
+    *reinterpret_cast<vec_t*>(dst + half) = y;
+  };
+  if (wave < 2) {
+    if (slot >= 0) {
+      const T* src = static_cast<const T*>(p.k) + row * p.k_stride + j0;
+      T* dst = static_cast<T*>(p.k_pages) + key_at(p, slot, 0) + j0;
+      const int64_t head = static_cast<int64_t>(D) << p.page_shift;
+#pragma unroll 4
+      for (int g = wave * HPW + hs; g < p.Hkv; g += 2 * HPW) turn(src + g * D, dst + g * head);
+    }
+  } else {
+    const T* v = static_cast<const T*>(p.v);
+    T* vp = static_cast<T*>(p.v_pages);
+    for (int u = 0; u < 8; ++u) {
+      const int s = near[7 + u];
+      if (s < 0) continue;
+      const int a = s & 7, l = 7 + u - a;            // the block's first row, as an index of near
+      bool whole = true;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) whole = whole && near[l + w] == s - a + w;
+      if (whole && a != 0) continue;                 // its first row writes it
+      for (int e = (wave - 2) * 64 + lane; e < p.Hkv * (D / 8); e += 128) {
+        const int g = e / (D / 8), d0 = (e % (D / 8)) * 8;
+        const T* src = v + static_cast<int64_t>(r0 + u) * p.v_stride + g * D + d0;
+        T* dst = vp + value_at(p, s, g) + d0 * 8;
+        if (whole) {
+          vec_t x[8];
+#pragma unroll
+          for (int w = 0; w < 8; ++w) x[w] = *reinterpret_cast<const vec_t*>(src + w * p.v_stride);
+#pragma unroll
+          for (int d = 0; d < 8; ++d) {
+            vec_t y;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) y[w] = x[w][d];
+            *reinterpret_cast<vec_t*>(dst + d * 8) = y;
+          }
+        } else {
+          const vec_t x = *reinterpret_cast<const vec_t*>(src);
+#pragma unroll
+          for (int d = 0; d < 8; ++d) dst[d * 8 + a] = x[d];
+        }
+      }
+    }
+  }
+  if (p.q && slot >= 0) {
+    const T* src = static_cast<const T*>(p.q) + row * p.q_stride + j0;
+    T* dst = static_cast<T*>(p.q_rot) + static_cast<int64_t>(row) * p.Hq * D + j0;
+#pragma unroll 4
+    for (int h = wave * HPW + hs; h < p.Hq; h += 4 * HPW) turn(src + h * D, dst + h * D);
+  }
+}
+
+template <typename T>
+void launch_append(const PagedAppendParams& p, hipStream_t s) {
+  if (p.num_rows <= kStepRows) {
+    constexpr int VE = Vec16<T>::N;
+    const int items = ((p.q ? p.Hq : 0) + p.Hkv) * (p.D / 2 / VE) + p.Hkv * (p.D / VE);
+    const int threads = std::min(1024, (items + 63) / 64 * 64);
+    append_row_kernel<T><<<p.num_rows, threads, 0, s>>>(p);
+    return;
+  }
+  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.num_rows) + 7) / 8);
+  if (p.D == 64) append_rows_kernel<T, 64><<<grid, 256, 0, s>>>(p);
+  else append_rows_kernel<T, 128><<<grid, 256, 0, s>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(int dtype, const PagedAppendParams& p, hipStream_t s) {
+  if (dtype == 0) launch_append<float>(p, s);
+  else launch_append<uint16_t>(p, s);
+  return hipGetLastError();
+}
+
+}  // namespace ippd

@@ -1,0 +1,479 @@
+// Attention of one new token per question over the paged cache: the plan's
+// pieces (paged_internal.h) in one launch, the join of their partial softmax
+// states in a second.
+//
+// With x_k = scale * q . K_k over the keys of the prompt's context and of the
+// question's own segment, out = sum_k e^(x_k) V_k / sum_k e^(x_k).  Any split of
+// the keys gives partial states (m = max x, l = sum e^(x - m), o = sum e^(x - m) V)
+// that join exactly: m = max m_i, l = sum e^(m_i - m) l_i, o likewise.
+//
+// A tile is 32 tokens, within one page (16-token pages: two).  Its page id is
+// read through the scalar cache a tile ahead, apart from the vector loads that
+// carry keys and values; an id outside the pool marks the piece's states as
+// bad (l = -1), its tiles are read from page 0, and the question gets no output.
+#include "ippd_device.h"
+#include "paged_internal.h"
+#include "tile_attend.h"
+
+namespace ippd {
+
+namespace {
+
+// Read-only words at a wave-uniform address, through the scalar cache.  (Their
+// waits are lgkmcnt's, so they leave the counts of the ring's DMAs alone.)
+typedef const int32_t __attribute__((address_space(4)))* scalar_words;
+__device__ __forceinline__ scalar_words scalars(const int32_t* p) { return (scalar_words)(uintptr_t)p; }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+struct Task {
+  int seq, len, rows, q, row, first, tiles;
+  __device__ __forceinline__ void load(const int32_t* plan, int64_t at) {
+    scalar_words w = scalars(plan + at);
+    seq = w[0]; len = w[1]; rows = w[2]; q = w[3]; row = w[4]; first = w[5]; tiles = w[6];
+  }
+};
+
+// One row block's running state.  l is the lane's own share of the row's sum of
+// weights, in fp32 and before the weights are rounded for the value product;
+// the four lanes of a row are summed at the end.
+template <int D>
+struct State {
+  f32x4_t o[D / 16];
+  float m, l;
+};
+
+template <int D>
+__device__ __forceinline__ void clear(State<D>& st) {
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) st.o[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  st.m = -INFINITY;
+  st.l = 0.f;
+}
+
+// Folds a tile's scores (lane (lg, lr): tokens 8 lg + 4 kb + v of row lr) into
+// the state and returns the weights as the value product's operand, rounded to
+// the cache's type (bf16: half a step, 2^-9, each; the sum keeps 32 bits).  The
+// offset m moves only when a score exceeds it by 2^8 in the exponent.
+template <typename T, int D>
+__device__ __forceinline__ typename Mfma<T>::Frag fold(const f32x4_t (&sc)[2], State<D>& st, float c) {
+  const float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                          fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+  if (wave_any((top - st.m) * c > kRescaleLog2)) {
+    const float m = fmaxf(st.m, xor32_max(xor16_max(top)));
+    const float alpha = fast_exp2((st.m - (m == -INFINITY ? 0.f : m)) * c);
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) st.o[db] *= alpha;
+    st.m = m;
+  }
+  const float cm = (st.m == -INFINITY ? 0.f : st.m) * c;
+  f32x8_t w;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) w[4 * kb + v] = fast_exp2(fmaf(sc[kb][v], c, -cm));
+  st.l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+  return Mfma<T>::from_f32(w);
+}
+
+// The state of a row block's rows to their slots; bad: marked.
+template <int D>
+__device__ __forceinline__ void publish(const PagedAttendParams& p, const State<D>& st, int64_t row, bool live, bool bad,
+                                        int lg) {
+  const float l = xor32_sum(xor16_sum(st.l));
+  if (!live) return;
+  float* dst = p.part_o + row * D + 4 * lg;
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4_t*>(dst + 16 * db) = st.o[db];
+  if (lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * row) = make_float2(st.m, bad ? -1.f : l);
+}
+
+// Query fragments of a row: lane (lg, lr) holds dims 32 ds + 8 lg + u.
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const PagedAttendParams& p, typename Mfma<T>::Frag (&qf)[D / 32], int q0, int r,
+                                           int g, int lg) {
+  const int i = p.plan[p.qlist + q0 + r / p.G];
+  const T* src = static_cast<const T*>(p.q_rot) + (static_cast<int64_t>(i) * p.Hq + g * p.G + r % p.G) * D + 8 * lg;
+#pragma unroll
+  for (int ds = 0; ds < D / 32; ++ds) qf[ds] = Mfma<T>::load(src + 32 * ds);
+}
+
+// Pages of the tiles of one sequence.  A tile lies in one page, or at 16 tokens
+// a page in two, of which the second may not exist: it then stands for the first.
+template <bool SMALL>
+struct Pages {
+  scalar_words table;
+  int shift, most, last;                             // pages of the pool; the sequence's last page
+  bool bad;
+  __device__ __forceinline__ void init(const PagedAttendParams& p, int seq, int len) {
+    table = scalars(p.block_table + static_cast<int64_t>(seq) * p.table_pages);
+    shift = SMALL ? 4 : p.page_shift;
+    most = p.num_pages;
+    last = (len - 1) >> shift;
+    bad = false;
+  }
+  // Page ids of tile t (the second is the first's unless SMALL).
+  __device__ __forceinline__ int2 of(int t) const {
+    const int a = (t << 5) >> shift;
+    const int x = table[min(a, last)];
+    return make_int2(x, SMALL ? table[min(a + 1, last)] : x);
+  }
+  __device__ __forceinline__ int2 checked(int2 id) {
+    const bool no = static_cast<uint32_t>(id.x) >= static_cast<uint32_t>(most) ||
+                    (SMALL && static_cast<uint32_t>(id.y) >= static_cast<uint32_t>(most));
+    bad = bad || no;
+    return no ? make_int2(0, 0) : id;
+  }
+};
+
+// Elements before page `id` of kv head g, and before its token t0 within the page.
+template <bool SMALL, int D>
+__device__ __forceinline__ int64_t page_at(const PagedAttendParams& p, int id, int g, int tile) {
+  const int shift = SMALL ? 4 : p.page_shift;
+  const int t0 = SMALL ? 0 : (tile << 5) & ((1 << shift) - 1);
+  return (((static_cast<int64_t>(id) * p.Hkv + g) << shift) + t0) * D;
+}
+
+// ---------------------------------------------------------------------------
+// Block line: a workgroup of four waves, 16 RB rows each, streams the piece's
+// tiles through the LDS ring of tile_attend.h, NS - 1 tiles ahead.  Every
+// fragment read from LDS serves RB row blocks.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int NS, bool SMALL>
+__device__ __forceinline__ void fetch(uint32_t stage, const PagedAttendParams& p, int2 id, int g, int tile, int wave, int lane,
+                                      const TileOffsets<T, D, kPagedWaves, NS>& to) {
+  using R = Ring<T, D, NS>;
+  constexpr int DPT = R::BLOCKS / kPagedWaves;
+  const int64_t a = page_at<SMALL, D>(p, id.x, g, tile);
+  const T* ka = static_cast<const T*>(p.k_pages) + a;
+  const T* va = static_cast<const T*>(p.v_pages) + a;
+  if constexpr (!SMALL) {
+#pragma unroll
+    for (int d = 0; d < DPT; ++d) {
+      const int q = wave + kPagedWaves * d;          // wave-uniform
+      dma16s(q < R::KBLOCKS ? ka : va, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
+    }
+  } else {
+    // the offsets are those of a whole tile: tokens 16 .. 31 sit at the second page's start
+    constexpr int HALF = 16 * D * R::E;
+    const int64_t b = page_at<SMALL, D>(p, id.y, g, tile);
+    const T* kb = static_cast<const T*>(p.k_pages) + b;
+    const T* vb = static_cast<const T*>(p.v_pages) + b;
+#pragma unroll
+    for (int d = 0; d < DPT; ++d) {
+      const int q = wave + kPagedWaves * d;
+      const bool second = to.off[d] >= HALF;
+      const char* base = reinterpret_cast<const char*>(q < R::KBLOCKS ? (second ? kb : ka) : (second ? vb : va));
+      dma16(base + (to.off[d] - (second ? HALF : 0)), stage + static_cast<uint32_t>(q) * 1024u);
+    }
+  }
+}
+
+template <typename T, int D, int NS, int RB>
+__device__ __forceinline__ void scores(const unsigned char* stage, const typename Mfma<T>::Frag (&qf)[RB][D / 32],
+                                       f32x4_t (&sc)[RB][2], int lr, int lg) {
+  using R = Ring<T, D, NS>;
+  using M = Mfma<T>;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int r = 16 * kb + lr, sw = (r >> R::KSH) & R::KMASK;
+    const unsigned char* row = stage + r * (R::CPR * 16);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) sc[rb][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ds = 0; ds < D / 32; ++ds) {
+      const int c0 = (8 * lg + 32 * ds) * R::E / 16;
+      const typename M::Frag kf = M::lds2(row + ((c0 ^ sw) * 16), row + (((c0 + 1) ^ sw) * 16));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sc[rb][kb] = M::mma(kf, qf[rb][ds], sc[rb][kb]);
+    }
+  }
+}
+
+template <typename T, int D, int NS, int RB>
+__device__ __forceinline__ void values(const unsigned char* stage, f32x4_t (&sc)[RB][2], State<D> (&st)[RB], int n, int lr,
+                                       int lg, float c) {
+  using R = Ring<T, D, NS>;
+  using M = Mfma<T>;
+  typename M::Frag pf[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    if (n < 32) mask_scores(sc[rb], n, lg);
+    pf[rb] = fold<T, D>(sc[rb], st[rb], c);
+  }
+  const int keep = min(max(n - 8 * lg, 0), 8);
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) {
+    const unsigned char* vp = stage + R::KBYTES + lg * R::VBLK + (16 * db + lr) * 8 * R::E;
+    typename M::Frag vf = M::lds2(vp, vp + 16);
+    if (n < 32) vf = M::keep_first(vf, keep);        // what lies past the end may be anything
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) st[rb].o[db] = M::mma(vf, pf[rb], st[rb].o[db]);
+  }
+}
+
+template <typename T, int D, int NS, int RB, bool SMALL>
+__device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned char* ring, int piece, int g, int wave, int lane) {
+  using R = Ring<T, D, NS>;
+  using M = Mfma<T>;
+  constexpr int DPT = R::BLOCKS / kPagedWaves;
+  const int lr = lane & 15, lg = lane >> 4;
+  const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
+  TileOffsets<T, D, kPagedWaves, NS> to;
+  to.init(wave, lane);
+  scalar_words pw = scalars(p.plan + p.piece1 + static_cast<int64_t>(piece) * kPieceWords);
+  int index = pw[0], tile = pw[1], left = pw[2];
+  while (left > 0) {
+    Task task;
+    task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
+    const int n = min(left, task.tiles - tile);
+    Pages<SMALL> pages;
+    pages.init(p, task.seq, task.len);
+    typename M::Frag qf[RB][D / 32];
+    bool live = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = 16 * (wave * RB + rb) + lr;
+      load_query<T, D>(p, qf[rb], task.q, min(r, task.rows - 1), g, lg);
+    }
+    live = 16 * wave * RB < task.rows;
+    State<D> st[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) clear(st[rb]);
+    int2 id = pages.of(tile);
+    for (int t = 0; t < NS - 1; ++t) {
+      if (t >= n) break;
+      const int2 next = pages.of(min(tile + t + 1, task.tiles - 1));
+      fetch<T, D, NS, SMALL>(lds + t * R::STAGE, p, pages.checked(id), g, tile + t, wave, lane, to);
+      id = next;
+    }
+    for (int t = 0; t < n; ++t) {
+      wait_tiles<DPT, NS - 2>(min(n - 1 - t, NS - 2));
+      __syncthreads();
+      const int tn = t + NS - 1;
+      if (tn < n) {
+        const int2 next = pages.of(min(tile + tn + 1, task.tiles - 1));
+        fetch<T, D, NS, SMALL>(lds + (tn % NS) * R::STAGE, p, pages.checked(id), g, tile + tn, wave, lane, to);
+        id = next;
+      }
+      if (live) {
+        f32x4_t sc[RB][2];
+        const unsigned char* stage = ring + (t % NS) * R::STAGE;
+        scores<T, D, NS, RB>(stage, qf, sc, lr, lg);
+        values<T, D, NS, RB>(stage, sc, st, min(32, task.len - 32 * (tile + t)), lr, lg, p.c);
+      }
+    }
+    __syncthreads();                                 // every wave is past the last tile
+    if (pages.bad && wave == 0 && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
+    const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = 16 * (wave * RB + rb) + lr;
+      publish<D>(p, st[rb], row + r, r < task.rows, pages.bad, lg);
+    }
+    left -= n;
+    tile = 0;
+    ++index;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Wave line: a wave streams its piece's tiles through its registers, the next
+// tile's keys and values in flight while it computes.
+// ---------------------------------------------------------------------------
+template <typename T, int D, bool SMALL>
+__device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece, int g, int lane) {
+  using M = Mfma<T>;
+  const int lr = lane & 15, lg = lane >> 4;
+  scalar_words pw = scalars(p.plan + p.piece2 + static_cast<int64_t>(piece) * kPieceWords);
+  int index = pw[0], tile = pw[1], left = pw[2];
+  // this lane's elements of a tile: keys of tokens tile_token(kb, lr), values of
+  // the 8 tokens of block lg; at 16 tokens a page the second page's start over
+  const int ktok = tile_token(0, lr), vtok = 8 * lg;
+  const bool k2 = SMALL && ktok >= 16, v2 = SMALL && vtok >= 16;
+  const int koff = (k2 ? ktok - 16 : ktok) * D + 8 * lg, voff = (v2 ? vtok - 16 : vtok) * D + 8 * lr;
+  while (left > 0) {
+    Task task;
+    task.load(p.plan, p.task2 + static_cast<int64_t>(index) * kTaskWords);
+    const int n = min(left, task.tiles - tile);
+    Pages<SMALL> pages;
+    pages.init(p, task.seq, task.len);
+    typename M::Frag qf[D / 32], kf[2][D / 32], vf[D / 16];
+    auto load_keys = [&](int2 id, int t) {
+      const int64_t a = page_at<SMALL, D>(p, id.x, g, t), b = SMALL ? page_at<SMALL, D>(p, id.y, g, t) : a;
+      const T* src = static_cast<const T*>(p.k_pages) + (k2 ? b : a) + koff;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ds = 0; ds < D / 32; ++ds) kf[kb][ds] = M::load(src + 4 * kb * D + 32 * ds);
+    };
+    auto load_values = [&](int2 id, int t) {
+      const int64_t a = page_at<SMALL, D>(p, id.x, g, t), b = SMALL ? page_at<SMALL, D>(p, id.y, g, t) : a;
+      const T* src = static_cast<const T*>(p.v_pages) + (v2 ? b : a) + voff;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) vf[db] = M::load(src + 128 * db);
+    };
+    int2 id = pages.checked(pages.of(tile));
+    load_query<T, D>(p, qf, task.q, min(lr, task.rows - 1), g, lg);
+    load_keys(id, tile);
+    load_values(id, tile);
+    int2 next = pages.of(min(tile + 1, task.tiles - 1));
+    State<D> st;
+    clear(st);
+    for (int t = 0; t < n; ++t) {
+      id = pages.checked(next);
+      next = pages.of(min(tile + t + 2, task.tiles - 1));
+      const int nt = min(tile + t + 1, task.tiles - 1);
+      f32x4_t sc[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        sc[kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ds = 0; ds < D / 32; ++ds) sc[kb] = M::mma(kf[kb][ds], qf[ds], sc[kb]);
+      }
+      if (t + 1 < n) load_keys(id, nt);
+      const int m = task.len - 32 * (tile + t);
+      if (m < 32) mask_scores(sc, m, lg);
+      const typename M::Frag pf = fold<T, D>(sc, st, p.c);
+      if (m < 32) {                                  // what lies past the end may be anything
+        const int keep = min(max(m - 8 * lg, 0), 8);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) vf[db] = M::keep_first(vf[db], keep);
+      }
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) st.o[db] = M::mma(vf[db], pf, st.o[db]);
+      if (t + 1 < n) load_values(id, nt);
+    }
+    if (pages.bad && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
+    const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
+    publish<D>(p, st, row + lr, lr < task.rows, pages.bad, lg);
+    left -= n;
+    tile = 0;
+    ++index;
+  }
+}
+
+// Whether the buffer holds a plan of this batch's sizes.
+__device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
+  scalar_words h = scalars(p.plan);
+  return h[0] == kPlanMagic && h[1] == p.B && h[2] == p.Nt && h[3] == p.W && h[4] == p.group_q && h[5] == p.G &&
+         h[8] == p.table_pages << p.page_shift;
+}
+
+template <typename T, int D, int NS, int RB, bool SMALL>
+__global__ __launch_bounds__(64 * kPagedWaves, sizeof(T) * D > 256 ? 1 : 2) void paged_attend_kernel(PagedAttendParams p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[NS * Ring<T, D, NS>::STAGE];
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (!plan_fits(p)) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(p.err_flag, kFlagBadLayout);
+    return;
+  }
+  const int n1 = scalars(p.plan)[6], n2 = scalars(p.plan)[7];
+  const int g = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv;
+  if (b < n1) {
+    block_piece<T, D, NS, RB, SMALL>(p, ring, b, g, wave, lane);
+    return;
+  }
+  const int piece = wave * (p.W - n1) + (b - n1);
+  if (piece < n2) wave_piece<T, D, SMALL>(p, piece, g, lane);
+}
+
+// ---------------------------------------------------------------------------
+// Join: a workgroup per (question, kv head).  An item is four dims of one head;
+// as many threads as there are share an item's states and are joined in LDS.
+// ---------------------------------------------------------------------------
+constexpr int kJoin = 256;
+
+struct Part {
+  float m, l;
+  f32x4_t o;
+};
+__device__ __forceinline__ void join(Part& a, float m, float l, const f32x4_t& o, float c) {
+  const float top = fmaxf(a.m, m), base = top == -INFINITY ? 0.f : top;
+  const float x = fast_exp2((a.m - base) * c), y = fast_exp2((m - base) * c);
+  a.l = a.l * x + l * y;
+  a.o = a.o * x + o * y;
+  a.m = top;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kJoin) void paged_join_kernel(PagedAttendParams p) {
+  __shared__ float part[kJoin * 6];
+  const int i = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;
+  if (!plan_fits(p)) return;
+  scalar_words w = scalars(p.plan + p.quest + static_cast<int64_t>(i) * kQuestionWords);
+  if (w[0] == 0) return;
+  const int row0 = w[1], n0 = w[2], step0 = w[3], row1 = w[4], n1 = w[5], n = n0 + n1;
+  const int items = p.G * (D / 4);
+  int phases = 1;
+  while (items * phases * 2 <= kJoin && phases < n) phases *= 2;
+  const int64_t base = static_cast<int64_t>(g) * p.rows;
+  for (int item0 = 0; item0 < items; item0 += kJoin / phases) {
+    const int per = min(items, kJoin / phases);
+    const int item = item0 + static_cast<int>(threadIdx.x) % per, ph = threadIdx.x / per;
+    const bool on = item < items && ph < phases;
+    const int h = item / (D / 4), d = (item % (D / 4)) * 4;
+    Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    bool bad = false;
+    if (on) {
+#pragma unroll 4
+      for (int k = ph; k < n; k += phases) {
+        const int64_t row = base + h + (k < n0 ? row0 + static_cast<int64_t>(k) * step0 : row1 + static_cast<int64_t>(k - n0) * p.G);
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row);
+        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d);
+        bad = bad || ml.y < 0.f;
+        join(a, ml.x, ml.y, o, p.c);
+      }
+    }
+    if (__syncthreads_or(bad)) return;               // a page outside the pool: no output
+    if (phases > 1) {
+      float* mine = part + threadIdx.x * 6;
+      mine[0] = a.m; mine[1] = a.l;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mine[2 + v] = a.o[v];
+      __syncthreads();
+      if (on && ph == 0)
+        for (int k = 1; k < phases; ++k) {
+          const float* x = part + (threadIdx.x + k * per) * 6;
+          join(a, x[0], x[1], f32x4_t{x[2], x[3], x[4], x[5]}, p.c);
+        }
+    }
+    if (on && ph == 0) {
+      const int64_t at = static_cast<int64_t>(i) * p.Hq + g * p.G + h;
+      const float inv = a.l == 0.f ? 0.f : 1.f / a.l;      // no keys at all: zeros, and lse -inf
+      T* dst = static_cast<T*>(p.out) + at * D + d;
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4_t*>(dst) = a.o * inv;
+      } else {
+        typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
+        u16x4_t y;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[v] = f32_to_bf16(a.o[v] * inv);
+        *reinterpret_cast<u16x4_t*>(dst) = y;
+      }
+      if (p.lse && d == 0) p.lse[at] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
+    }
+  }
+}
+
+template <typename T, int D, int NS, int RB>
+hipError_t launch(const PagedAttendParams& p, hipStream_t s) {
+  const unsigned grid = static_cast<unsigned>(p.W) * p.Hkv;
+  if (p.page_shift == 4) paged_attend_kernel<T, D, NS, RB, true><<<grid, 64 * kPagedWaves, 0, s>>>(p);
+  else paged_attend_kernel<T, D, NS, RB, false><<<grid, 64 * kPagedWaves, 0, s>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  paged_join_kernel<T, D><<<static_cast<unsigned>(p.Nt) * p.Hkv, kJoin, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attend(int dtype, int D, int rb, const PagedAttendParams& p, hipStream_t s) {
+  if (dtype == 0) return D == 64 ? launch<float, 64, 5, 1>(p, s) : launch<float, 128, 4, 1>(p, s);
+  if (D == 64) return rb == 2 ? launch<uint16_t, 64, 5, 2>(p, s) : launch<uint16_t, 64, 5, 1>(p, s);
+  return rb == 2 ? launch<uint16_t, 128, 5, 2>(p, s) : launch<uint16_t, 128, 5, 1>(p, s);
+}
+
+}  // namespace ippd
