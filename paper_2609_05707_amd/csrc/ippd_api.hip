@@ -385,7 +385,7 @@ ippd_status_t ippd_paged_plan(const ippd_paged_batch_t* bt, void* plan, size_t p
   ippd::PagedPlanParams p;
   p.plan = static_cast<int32_t*>(plan);
   p.q_start = bt->q_start; p.seq_len = bt->seq_len; p.active = bt->active; p.err_flag = bt->err_flag;
-  p.B = bt->num_prompts; p.Nt = bt->num_questions; p.G = s.G; p.W = s.W; p.group_q = s.group_q;
+  p.B = bt->num_prompts; p.Nt = bt->num_questions; p.G = s.G; p.W = s.W; p.waves = s.waves; p.group_q = s.group_q;
   p.max_questions = bt->max_questions;
   p.max_len = bt->table_pages * bt->page_tokens;
   p.piece1 = s.piece1; p.piece2 = s.piece2; p.task1 = s.task1; p.task2 = s.task2; p.quest = s.quest;
@@ -424,7 +424,7 @@ ippd_status_t ippd_paged_decode_attention(const ippd_paged_batch_t* bt, const ip
   p.table_pages = bt->table_pages;
   p.scale = softmax_scale(bt);
   p.c = p.scale * 1.4426950408889634f;
-  return hip_status(ippd::launch_paged_attend(bt->dtype, bt->head_dim, s.rb, p, stream));
+  return hip_status(ippd::launch_paged_attend(bt->dtype, bt->head_dim, s.waves, s.rb, p, stream));
 }
 
 const char* ippd_status_string(ippd_status_t s) {

@@ -136,22 +136,23 @@ __device__ __forceinline__ int64_t page_at(const PagedAttendParams& p, int id, i
 }
 
 // ---------------------------------------------------------------------------
-// Block line: a workgroup of four waves, 16 RB rows each, streams the piece's
-// tiles through the LDS ring of tile_attend.h, NS - 1 tiles ahead.  Every
-// fragment read from LDS serves RB row blocks.
+// Block line: a workgroup of NW waves, up to RB 16-row blocks each, streams the
+// piece's tiles through the LDS ring of tile_attend.h, NS - 1 tiles ahead.
+// Every fragment read from LDS serves the wave's row blocks.  Block j of wave w
+// holds rows 16 (NW j + w) .., so that few rows spread over all four SIMDs.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int NS, bool SMALL>
+template <typename T, int D, int NW, int NS, bool SMALL>
 __device__ __forceinline__ void fetch(uint32_t stage, const PagedAttendParams& p, int2 id, int g, int tile, int wave, int lane,
-                                      const TileOffsets<T, D, kPagedWaves, NS>& to) {
+                                      const TileOffsets<T, D, NW, NS>& to) {
   using R = Ring<T, D, NS>;
-  constexpr int DPT = R::BLOCKS / kPagedWaves;
+  constexpr int DPT = R::BLOCKS / NW;
   const int64_t a = page_at<SMALL, D>(p, id.x, g, tile);
   const T* ka = static_cast<const T*>(p.k_pages) + a;
   const T* va = static_cast<const T*>(p.v_pages) + a;
   if constexpr (!SMALL) {
 #pragma unroll
     for (int d = 0; d < DPT; ++d) {
-      const int q = wave + kPagedWaves * d;          // wave-uniform
+      const int q = wave + NW * d;                   // wave-uniform
       dma16s(q < R::KBLOCKS ? ka : va, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
     }
   } else {
@@ -162,7 +163,7 @@ __device__ __forceinline__ void fetch(uint32_t stage, const PagedAttendParams& p
     const T* vb = static_cast<const T*>(p.v_pages) + b;
 #pragma unroll
     for (int d = 0; d < DPT; ++d) {
-      const int q = wave + kPagedWaves * d;
+      const int q = wave + NW * d;
       const bool second = to.off[d] >= HALF;
       const char* base = reinterpret_cast<const char*>(q < R::KBLOCKS ? (second ? kb : ka) : (second ? vb : va));
       dma16(base + (to.off[d] - (second ? HALF : 0)), stage + static_cast<uint32_t>(q) * 1024u);
@@ -170,6 +171,7 @@ __device__ __forceinline__ void fetch(uint32_t stage, const PagedAttendParams& p
   }
 }
 
+// Raw scores of a stage's keys.
 template <typename T, int D, int NS, int RB>
 __device__ __forceinline__ void scores(const unsigned char* stage, const typename Mfma<T>::Frag (&qf)[RB][D / 32],
                                        f32x4_t (&sc)[RB][2], int lr, int lg) {
@@ -191,6 +193,7 @@ __device__ __forceinline__ void scores(const unsigned char* stage, const typenam
   }
 }
 
+// Folds a tile's scores and adds the weights times its values (n valid tokens).
 template <typename T, int D, int NS, int RB>
 __device__ __forceinline__ void values(const unsigned char* stage, f32x4_t (&sc)[RB][2], State<D> (&st)[RB], int n, int lr,
                                        int lg, float c) {
@@ -213,14 +216,119 @@ __device__ __forceinline__ void values(const unsigned char* stage, f32x4_t (&sc)
   }
 }
 
-template <typename T, int D, int NS, int RB, bool SMALL>
-__device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned char* ring, int piece, int g, int wave, int lane) {
+// A step of the loop: the scores sn of the next tile (keys at stk) while this
+// one's (sc, values at stv, all 32 tokens valid) are folded.  The key reads go
+// out first and the softmax covers them, the score products cover the value
+// reads; the wave's priority is up over its products, so that they issue back
+// to back while the SIMD's other wave runs its softmax.
+template <typename T, int D, int NS, int RB>
+__device__ __forceinline__ void step(const unsigned char* stk, const unsigned char* stv,
+                                     const typename Mfma<T>::Frag (&qf)[RB][D / 32], f32x4_t (&sc)[RB][2],
+                                     f32x4_t (&sn)[RB][2], State<D> (&st)[RB], int lr, int lg, float c) {
   using R = Ring<T, D, NS>;
   using M = Mfma<T>;
-  constexpr int DPT = R::BLOCKS / kPagedWaves;
+  typename M::Frag kf[2][D / 32], vf[D / 16], pf[RB];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int r = 16 * kb + lr, sw = (r >> R::KSH) & R::KMASK;
+    const unsigned char* row = stk + r * (R::CPR * 16);
+#pragma unroll
+    for (int ds = 0; ds < D / 32; ++ds) {
+      const int c0 = (8 * lg + 32 * ds) * R::E / 16;
+      kf[kb][ds] = M::lds2(row + ((c0 ^ sw) * 16), row + (((c0 + 1) ^ sw) * 16));
+    }
+  }
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) pf[rb] = fold<T, D>(sc[rb], st[rb], c);
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) sn[rb][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ds = 0; ds < D / 32; ++ds)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sn[rb][kb] = M::mma(kf[kb][ds], qf[rb][ds], sn[rb][kb]);
+  }
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) {
+    const unsigned char* vp = stv + R::KBYTES + lg * R::VBLK + (16 * db + lr) * 8 * R::E;
+    vf[db] = M::lds2(vp, vp + 16);
+  }
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) st[rb].o[db] = M::mma(vf[db], pf[rb], st[rb].o[db]);
+  __builtin_amdgcn_s_setprio(0);
+}
+
+// n tiles of a task from `tile` on, for a wave with RL row blocks (0: it only
+// fetches).  Waves of a workgroup differ in RL and meet at the same barriers.
+template <typename T, int D, int NW, int NS, int RL, bool SMALL>
+__device__ __forceinline__ void stream(const PagedAttendParams& p, unsigned char* ring, const Task& task, int g, int tile,
+                                       int n, int64_t row, Pages<SMALL>& pages, int wave, int lane,
+                                       const TileOffsets<T, D, NW, NS>& to) {
+  using R = Ring<T, D, NS>;
+  using M = Mfma<T>;
+  constexpr int DPT = R::BLOCKS / NW, RB = RL ? RL : 1;
   const int lr = lane & 15, lg = lane >> 4;
   const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
-  TileOffsets<T, D, kPagedWaves, NS> to;
+  typename M::Frag qf[RB][D / 32];
+  State<D> st[RB];
+  if constexpr (RL > 0) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      load_query<T, D>(p, qf[rb], task.q, min(16 * (NW * rb + wave) + lr, task.rows - 1), g, lg);
+      clear(st[rb]);
+    }
+  }
+  int2 id = pages.of(tile);
+  auto next_fetch = [&](int t) {                     // tile t of the n
+    const int2 next = pages.of(min(tile + t + 1, task.tiles - 1));
+    fetch<T, D, NW, NS, SMALL>(lds + (t % NS) * R::STAGE, p, pages.checked(id), g, tile + t, wave, lane, to);
+    id = next;
+  };
+  for (int t = 0; t < NS - 1 && t < n; ++t) next_fetch(t);
+  const int last = n - 1;
+  // tile t is folded in step t, whose barrier also says that every wave is past
+  // step t - 1; the stage of tile t - 1 then takes tile t + NS - 1.  Steps in
+  // pairs, so that the two sets of scores swap places without copies.
+  f32x4_t sa[RB][2], sb[RB][2];
+  wait_tiles<DPT, NS - 2>(min(last, NS - 2));
+  __syncthreads();
+  if constexpr (RL > 0) scores<T, D, NS, RB>(ring, qf, sa, lr, lg);
+  auto half = [&](int t, f32x4_t (&now)[RB][2], f32x4_t (&then)[RB][2]) {
+    wait_tiles<DPT, NS - 3>(min(last - t - 1, NS - 3));
+    __syncthreads();
+    if (t + NS - 1 <= last) next_fetch(t + NS - 1);
+    if constexpr (RL > 0)
+      step<T, D, NS, RB>(ring + ((t + 1) % NS) * R::STAGE, ring + (t % NS) * R::STAGE, qf, now, then, st, lr, lg, p.c);
+  };
+  int t = 0;
+  for (; t + 2 <= last; t += 2) {
+    half(t, sa, sb);
+    half(t + 1, sb, sa);
+  }
+  const int tail = min(32, task.len - 32 * (tile + last));
+  const unsigned char* end = ring + (last % NS) * R::STAGE;
+  if (t < last) {
+    half(t, sa, sb);
+    if constexpr (RL > 0) values<T, D, NS, RB>(end, sb, st, tail, lr, lg, p.c);
+  } else {
+    if constexpr (RL > 0) values<T, D, NS, RB>(end, sa, st, tail, lr, lg, p.c);
+  }
+  if constexpr (RL > 0) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = 16 * (NW * rb + wave) + lr;
+      publish<D>(p, st[rb], row + r, r < task.rows, pages.bad, lg);
+    }
+  }
+}
+
+template <typename T, int D, int NW, int NS, int RB, bool SMALL>
+__device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned char* ring, int piece, int g, int wave, int lane) {
+  TileOffsets<T, D, NW, NS> to;
   to.init(wave, lane);
   scalar_words pw = scalars(p.plan + p.piece1 + static_cast<int64_t>(piece) * kPieceWords);
   int index = pw[0], tile = pw[1], left = pw[2];
@@ -230,51 +338,18 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
     const int n = min(left, task.tiles - tile);
     Pages<SMALL> pages;
     pages.init(p, task.seq, task.len);
-    typename M::Frag qf[RB][D / 32];
-    bool live = false;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = 16 * (wave * RB + rb) + lr;
-      load_query<T, D>(p, qf[rb], task.q, min(r, task.rows - 1), g, lg);
-    }
-    live = 16 * wave * RB < task.rows;
-    State<D> st[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) clear(st[rb]);
-    int2 id = pages.of(tile);
-    for (int t = 0; t < NS - 1; ++t) {
-      if (t >= n) break;
-      const int2 next = pages.of(min(tile + t + 1, task.tiles - 1));
-      fetch<T, D, NS, SMALL>(lds + t * R::STAGE, p, pages.checked(id), g, tile + t, wave, lane, to);
-      id = next;
-    }
-    for (int t = 0; t < n; ++t) {
-      wait_tiles<DPT, NS - 2>(min(n - 1 - t, NS - 2));
-      __syncthreads();
-      const int tn = t + NS - 1;
-      if (tn < n) {
-        const int2 next = pages.of(min(tile + tn + 1, task.tiles - 1));
-        fetch<T, D, NS, SMALL>(lds + (tn % NS) * R::STAGE, p, pages.checked(id), g, tile + tn, wave, lane, to);
-        id = next;
-      }
-      if (live) {
-        f32x4_t sc[RB][2];
-        const unsigned char* stage = ring + (t % NS) * R::STAGE;
-        scores<T, D, NS, RB>(stage, qf, sc, lr, lg);
-        values<T, D, NS, RB>(stage, sc, st, min(32, task.len - 32 * (tile + t)), lr, lg, p.c);
-      }
-    }
-    __syncthreads();                                 // every wave is past the last tile
-    if (pages.bad && wave == 0 && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
     const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = 16 * (wave * RB + rb) + lr;
-      publish<D>(p, st[rb], row + r, r < task.rows, pages.bad, lg);
-    }
+    if (RB == 2 && 16 * (NW + wave) < task.rows)
+      stream<T, D, NW, NS, RB, SMALL>(p, ring, task, g, tile, n, row, pages, wave, lane, to);
+    else if (16 * wave < task.rows)
+      stream<T, D, NW, NS, 1, SMALL>(p, ring, task, g, tile, n, row, pages, wave, lane, to);
+    else
+      stream<T, D, NW, NS, 0, SMALL>(p, ring, task, g, tile, n, row, pages, wave, lane, to);
+    if (pages.bad && wave == 0 && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
     left -= n;
     tile = 0;
     ++index;
+    __syncthreads();                                 // every wave is past the last tile
   }
 }
 
@@ -361,8 +436,8 @@ __device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
          h[8] == p.table_pages << p.page_shift;
 }
 
-template <typename T, int D, int NS, int RB, bool SMALL>
-__global__ __launch_bounds__(64 * kPagedWaves, sizeof(T) * D > 256 ? 1 : 2) void paged_attend_kernel(PagedAttendParams p) {
+template <typename T, int D, int NW, int NS, int RB, bool SMALL>
+__global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendParams p) {
   __shared__ __attribute__((aligned(1024))) unsigned char ring[NS * Ring<T, D, NS>::STAGE];
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (!plan_fits(p)) {
@@ -372,7 +447,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, sizeof(T) * D > 256 ? 1 : 2) void
   const int n1 = scalars(p.plan)[6], n2 = scalars(p.plan)[7];
   const int g = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv;
   if (b < n1) {
-    block_piece<T, D, NS, RB, SMALL>(p, ring, b, g, wave, lane);
+    block_piece<T, D, NW, NS, RB, SMALL>(p, ring, b, g, wave, lane);
     return;
   }
   const int piece = wave * (p.W - n1) + (b - n1);
@@ -457,11 +532,11 @@ __global__ __launch_bounds__(kJoin) void paged_join_kernel(PagedAttendParams p) 
   }
 }
 
-template <typename T, int D, int NS, int RB>
+template <typename T, int D, int NW, int NS, int RB>
 hipError_t launch(const PagedAttendParams& p, hipStream_t s) {
   const unsigned grid = static_cast<unsigned>(p.W) * p.Hkv;
-  if (p.page_shift == 4) paged_attend_kernel<T, D, NS, RB, true><<<grid, 64 * kPagedWaves, 0, s>>>(p);
-  else paged_attend_kernel<T, D, NS, RB, false><<<grid, 64 * kPagedWaves, 0, s>>>(p);
+  if (p.page_shift == 4) paged_attend_kernel<T, D, NW, NS, RB, true><<<grid, 64 * NW, 0, s>>>(p);
+  else paged_attend_kernel<T, D, NW, NS, RB, false><<<grid, 64 * NW, 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   paged_join_kernel<T, D><<<static_cast<unsigned>(p.Nt) * p.Hkv, kJoin, 0, s>>>(p);
@@ -470,10 +545,14 @@ hipError_t launch(const PagedAttendParams& p, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_paged_attend(int dtype, int D, int rb, const PagedAttendParams& p, hipStream_t s) {
-  if (dtype == 0) return D == 64 ? launch<float, 64, 5, 1>(p, s) : launch<float, 128, 4, 1>(p, s);
-  if (D == 64) return rb == 2 ? launch<uint16_t, 64, 5, 2>(p, s) : launch<uint16_t, 64, 5, 1>(p, s);
-  return rb == 2 ? launch<uint16_t, 128, 5, 2>(p, s) : launch<uint16_t, 128, 5, 1>(p, s);
+hipError_t launch_paged_attend(int dtype, int D, int waves, int rb, const PagedAttendParams& p, hipStream_t s) {
+  if (dtype == 0) return D == 64 ? launch<float, 64, 4, 5, 1>(p, s) : launch<float, 128, 8, 4, 1>(p, s);
+  if (D == 64) {
+    if (waves == 8) return launch<uint16_t, 64, 8, 9, 2>(p, s);
+    return rb == 2 ? launch<uint16_t, 64, 4, 9, 2>(p, s) : launch<uint16_t, 64, 4, 9, 1>(p, s);
+  }
+  if (waves == 8) return launch<uint16_t, 128, 8, 9, 2>(p, s);
+  return rb == 2 ? launch<uint16_t, 128, 4, 5, 2>(p, s) : launch<uint16_t, 128, 4, 5, 1>(p, s);
 }
 
 }  // namespace ippd

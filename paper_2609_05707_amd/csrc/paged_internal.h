@@ -18,7 +18,6 @@
 
 namespace ippd {
 
-constexpr int kPagedWaves = 4;            // waves of an attention workgroup
 constexpr int kPlanMagic = 0x49504450;    // first word of a plan
 constexpr int kPlanHeader = 64;           // words of its header
 constexpr int kPieceWords = 4;            // task, first tile within it, tiles of the piece, 0
@@ -31,6 +30,7 @@ constexpr int kPromptWords = 4;           // kind (0 none, 1 block line, 2 wave 
 struct PagedShape {
   int G, page_shift;
   int W;                                  // workgroups per kv head
+  int waves;                              // waves of a workgroup: 4, two workgroups on a compute unit, or 8
   int rb;                                 // 16-row blocks per wave of a block-line piece
   int group_q;                            // questions of a block-line row group (0: no block line)
   int64_t rows;                           // partial states per kv head
@@ -58,7 +58,7 @@ struct PagedAppendParams {
 struct PagedPlanParams {
   int32_t* plan;
   const int32_t* q_start; const int32_t* seq_len; const uint8_t* active; int32_t* err_flag;
-  int B, Nt, G, W, group_q, max_questions;
+  int B, Nt, G, W, waves, group_q, max_questions;
   int max_len;                            // table_pages * page_tokens
   int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank;
 };
@@ -77,6 +77,6 @@ struct PagedAttendParams {
 hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s);
 hipError_t launch_paged_append(int dtype, const PagedAppendParams& p, hipStream_t s);
 hipError_t launch_paged_plan(const PagedPlanParams& p, hipStream_t s);
-hipError_t launch_paged_attend(int dtype, int D, int rb, const PagedAttendParams& p, hipStream_t s);
+hipError_t launch_paged_attend(int dtype, int D, int waves, int rb, const PagedAttendParams& p, hipStream_t s);
 
 }  // namespace ippd

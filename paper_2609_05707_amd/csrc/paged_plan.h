@@ -43,23 +43,24 @@ inline int page_shift_of(int page_tokens) {
   return s;
 }
 
-// Attention workgroups resident on the chip at once, which the lines are cut
-// for: two on each of 256 compute units, one at fp32 with head_dim 128, whose
-// key ring takes most of a compute unit's LDS.  (A constant, not a device
-// query: sizes then depend on the batch fields only.)
-inline int paged_slots(const ippd_paged_batch_t* bt) {
-  return bt->dtype == IPPD_DTYPE_F32 && bt->head_dim == 128 ? 256 : 512;
-}
+// (A constant of MI355X, not a device query: sizes then depend on the batch
+// fields only.)
+constexpr int kPagedComputeUnits = 256;
 
 inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   PagedShape s;
   s.G = bt->num_q_heads / bt->num_kv_heads;
   s.page_shift = page_shift_of(bt->page_tokens);
-  s.W = std::max(2, paged_slots(bt) / bt->num_kv_heads);
+  const bool bf16 = bt->dtype == IPPD_DTYPE_BF16;
   const int most = bt->max_questions * s.G;
-  s.rb = bt->dtype == IPPD_DTYPE_BF16 && most > 64 ? 2 : 1;
-  s.group_q = most > 16 ? 16 * kPagedWaves * s.rb / s.G : 0;
-  const int64_t nt = bt->num_questions, b = bt->num_prompts, w1 = s.W, w2 = static_cast<int64_t>(kPagedWaves) * s.W;
+  // Eight waves, and a compute unit's LDS to themselves, where a context has more
+  // rows than four waves hold (a second row group would stream it again), and for
+  // fp32 at head_dim 128, whose ring leaves no room for a second workgroup.
+  s.waves = (bf16 ? most > 128 : bt->head_dim == 128) ? 8 : 4;
+  s.rb = bf16 && most > 64 ? 2 : 1;
+  s.W = std::max(2, kPagedComputeUnits * (s.waves == 8 ? 1 : 2) / bt->num_kv_heads);
+  s.group_q = most > 16 ? 16 * s.waves * s.rb / s.G : 0;
+  const int64_t nt = bt->num_questions, b = bt->num_prompts, w1 = s.W, w2 = w1 * s.waves;
   // every row of a task once, and again for each cut of a line that falls inside the task
   s.rows = 2 * nt * s.G + (s.group_q ? w1 * s.group_q * s.G : 0) + w2 * 16;
   int64_t at = kPlanHeader;

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     const int64_t share = (W1 * p.W + (W1 + T2) / 2) / (W1 + T2);
     n1 = static_cast<int>(min(max(min(share, (T1 + 3) / 4), static_cast<int64_t>(1)), most));
   }
-  if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(kPagedWaves) * (p.W - n1), (T2 + 1) / 2));
+  if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(p.waves) * (p.W - n1), (T2 + 1) / 2));
   const Line line1(T1, n1), line2(T2, n2);
 
   // block line: contexts, their active questions in even groups
