@@ -36,12 +36,20 @@ float softmax_scale(const B* bt) {
   return bt->scale > 0.f ? bt->scale : 1.0f / sqrtf(static_cast<float>(bt->head_dim));
 }
 
-// theta_j = base^(-2j/D) in fp64, the rotation frequencies of pair j.
+// theta_j = base^(-2j/D) in fp64, the rotation frequencies of pair j.  A thread
+// keeps its last table with the base and size it is of: 64 powers cost 1 us.
 template <typename B>
 void fill_inv_freq(const B* bt, double* out) {
-  const int half = bt->head_dim / 2;
-  for (int j = 0; j < ippd::kMaxHalfDim; ++j)
-    out[j] = j < half ? pow(bt->rope_base, -2.0 * j / bt->head_dim) : 0.0;
+  thread_local double base = 0.0, table[ippd::kMaxHalfDim];
+  thread_local int dim = 0;
+  if (base != bt->rope_base || dim != bt->head_dim) {
+    const int half = bt->head_dim / 2;
+    for (int j = 0; j < ippd::kMaxHalfDim; ++j)
+      table[j] = j < half ? pow(bt->rope_base, -2.0 * j / bt->head_dim) : 0.0;
+    base = bt->rope_base;
+    dim = bt->head_dim;
+  }
+  memcpy(out, table, sizeof table);
 }
 
 ippd_status_t hip_status(hipError_t e) {

@@ -23,7 +23,8 @@ constexpr int kPlanHeader = 64;           // words of its header
 constexpr int kPieceWords = 4;            // task, first tile within it, tiles of the piece, 0
 constexpr int kTaskWords = 8;             // sequence, tokens, rows, first active question, first state row, first piece, tiles, states (pieces)
 constexpr int kQuestionWords = 8;         // served, context state row, states, rows a state; segment state row, states; 0, 0
-constexpr int kPromptWords = 4;           // kind (0 none, 1 block line, 2 wave line), first task, questions a group, rank of its first question
+constexpr int kPromptWords = 4;           // kind (0 none, 1 block line, 2 wave line); first task and questions a
+                                          // group, or first state row and states; rank of its first question
 
 // Sizes of a batch's plan and of its partial states: functions of the batch's
 // host fields only.

@@ -21,36 +21,79 @@ constexpr int kFusedRows = 8192;
 
 constexpr int kFlagPagesExhausted = 4;
 
-// Sum of v over the lanes below this one's and, in the last lane, over all.
+// v of the lane that a DPP control names, 0 where there is none or row_mask leaves the row out.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t dpp(int64_t v) {
+  const uint32_t lo = dpp<CTRL, ROWS>(static_cast<int>(v)), hi = dpp<CTRL, ROWS>(static_cast<int>(v >> 32));
+  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+// Sum over this lane and those below it: four shifts within rows of 16 lanes,
+// then the rows' sums passed on (row_shr 1, 2, 4, 8, row_bcast 15 and 31).
 template <typename V>
 __device__ __forceinline__ V wave_inclusive(V v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const V u = __shfl_up(v, d, 64);
-    if (lane >= d) v += u;
-  }
+  v += dpp<0x111, 0xF>(v);
+  v += dpp<0x112, 0xF>(v);
+  v += dpp<0x114, 0xF>(v);
+  v += dpp<0x118, 0xF>(v);
+  v += dpp<0x142, 0xA>(v);
+  v += dpp<0x143, 0xC>(v);
   return v;
 }
 
-// Exclusive prefix sum over the workgroup; total: the sum over all threads.
+// Sum over this lane and those below it in its row of 16.
 template <typename V>
-__device__ __forceinline__ V block_exclusive(V v, V* lds, V& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const V inc = wave_inclusive(v);
-  __syncthreads();                                   // the previous use of lds is over
-  if (lane == 63) lds[wave] = inc;
-  __syncthreads();
-  V before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const V x = lds[w];
-    before += w < wave ? x : 0;
-    all += x;
-  }
-  total = all;
-  return before + inc - v;
+__device__ __forceinline__ V row_inclusive(V v) {
+  v += dpp<0x111, 0xF>(v);
+  v += dpp<0x112, 0xF>(v);
+  v += dpp<0x114, 0xF>(v);
+  v += dpp<0x118, 0xF>(v);
+  return v;
 }
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+  const uint32_t lo = lane_value(static_cast<int>(v), lane), hi = lane_value(static_cast<int>(v >> 32), lane);
+  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
+// Exclusive prefix sums over the workgroup, and their totals.  The waves' sums
+// meet in LDS and every wave adds them up in a row of lanes (kWaves is 16).  Two
+// buffers are used in turn: one barrier a sum, and the next sum's barrier
+// separates a buffer's readers from its next writers.
+struct Scan {
+  int64_t (*lds)[kWaves][2];
+  int turn;
+  template <typename V>
+  __device__ __forceinline__ V place(V inc, int col, int64_t (*at)[2], V& total) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const V up = row_inclusive<V>(static_cast<V>(at[threadIdx.x & 15][col]));
+    total = lane_value(up, 15);
+    return (wave ? lane_value(up, wave - 1) : V(0)) + inc;
+  }
+  __device__ __forceinline__ void operator()(int64_t& a, int64_t& b, int64_t& ta, int64_t& tb) {
+    const int64_t ia = wave_inclusive(a), ib = wave_inclusive(b);
+    int64_t (*at)[2] = lds[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) {
+      at[threadIdx.x >> 6][0] = ia;
+      at[threadIdx.x >> 6][1] = ib;
+    }
+    __syncthreads();
+    a = place(ia, 0, at, ta) - a;
+    b = place(ib, 1, at, tb) - b;
+  }
+  __device__ __forceinline__ int operator()(int v, int& total) {
+    const int inc = wave_inclusive(v);
+    int64_t (*at)[2] = lds[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) at[threadIdx.x >> 6][0] = inc;
+    __syncthreads();
+    return place(inc, 0, at, total) - v;
+  }
+};
+static_assert(kWaves == 16, "the waves' sums are added up in a row of lanes");
 
 // The last index of a non-decreasing array of n entries that is <= x (0 if none).
 template <typename A>
@@ -98,8 +141,7 @@ __device__ __forceinline__ void write_row(const ReserveParams& p, int row, int s
 
 template <bool ROWS>
 __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
-  __shared__ int64_t sums64[kWaves];
-  __shared__ int sums[kWaves];
+  __shared__ int64_t sums[2][kWaves][2];
   __shared__ int first[kThreads];                    // pages before the sequence, in this window
   __shared__ int from[kThreads];                     // its first page moved
   __shared__ int taken;
@@ -108,6 +150,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
   const int tid = threadIdx.x, S = p.B + p.Nt, sh = p.page_shift;
   const int64_t cap = static_cast<int64_t>(p.table_pages) << sh;
   const int f = *p.free_count;
+  Scan scan = {sums, 0};
   if (tid == 0) taken = 0;
 
   // checks, and the pages given back
@@ -124,8 +167,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
     bad = bad || qb < qa || (b == 0 && qa != 0) || (b == p.B - 1 && qb != p.Nt);
     if constexpr (ROWS) q0[b] = qa;
   }
-  int64_t total_back;
-  block_exclusive<int64_t>(back, sums64, total_back);
+  int64_t total_back, none = 0, zero;
+  scan(back, none, total_back, zero);
   bad = __syncthreads_or(bad || total_back > p.num_pages - f);
   if (bad) {                                         // nothing is moved: no row of the call is served
     if (tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
@@ -154,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
         }
       }
       int total;
-      const int ex = block_exclusive<int>(n, sums, total);
+      const int ex = scan(n, total);
       first[tid] = ex;
       from[tid] = keep;
       __syncthreads();
@@ -188,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
       }
     }
     int total;
-    const int ex = block_exclusive<int>(need, sums, total);
+    const int ex = scan(need, total);
     // (the sums need no 64 bits: the rows, and with them the new tokens, number
     // fewer than 2^31)
     const int upto = carry + ex + need;
@@ -250,109 +293,132 @@ __global__ __launch_bounds__(256) void rows_kernel(ReserveParams p) {
 
 // ---------------------------------------------------------------------------
 // Plan of a decode step's attention: see paged_internal.h for the lines.
+//
+// The two lines' tasks are numbered, placed and given their states by prefix
+// sums over prompts and questions.  Up to kPlanLds sequences everything that is
+// read twice (lengths, offsets, ranks, prompts) is in LDS and the call takes
+// two round trips to memory, the inputs in and the plan out; larger batches
+// keep it in the plan.
 // ---------------------------------------------------------------------------
+constexpr int kPlanLds = 1024;
+
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  const uint64_t x = a, y = b;
+  if (((x | y) >> 32) == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(y);
+  return static_cast<int64_t>(x / y);
+}
+
 // A line of T tiles cut into n <= T pieces, the first T % n of them one tile longer.
 struct Line {
-  int64_t T, size, longer;                           // tiles; of a short piece; pieces that are longer
+  int64_t size, longer, edge;                        // tiles of a short piece; pieces that are longer, and where they end
   int n;
-  __device__ __forceinline__ Line(int64_t tiles, int pieces) : T(tiles), size(pieces ? tiles / pieces : 0), longer(pieces ? tiles % pieces : 0), n(pieces) {}
+  __device__ __forceinline__ Line(int64_t tiles, int pieces) : size(0), longer(0), edge(0), n(pieces) {
+    if (pieces == 0) return;
+    size = quotient(tiles, pieces);
+    longer = tiles - size * pieces;
+    edge = longer * (size + 1);
+  }
   __device__ __forceinline__ int64_t start(int p) const { return p * size + (p < longer ? p : longer); }
   __device__ __forceinline__ int piece_of(int64_t x) const {
-    const int64_t edge = longer * (size + 1);
-    return static_cast<int>(x < edge ? x / (size + 1) : longer + (x - edge) / size);
+    return static_cast<int>(x < edge ? quotient(x, size + 1) : longer + quotient(x - edge, size));
   }
 };
 
-// A task of `tiles` > 0 tiles from `at` on the line: its record, and the
-// records of the pieces that begin inside it.
+// A task of `tiles` > 0 tiles from `at` on the line, in pieces first .. first + states - 1:
+// its record, and the records of the pieces that begin inside it.
 __device__ __forceinline__ void write_task(int32_t* plan, int64_t tasks, int64_t pieces, const Line& line, int index,
-                                           int64_t at, int tiles, int seq, int len, int rows, int q, int row, int states) {
-  const int first = line.piece_of(at);
+                                           int64_t at, int tiles, int seq, int len, int rows, int q, int row, int first,
+                                           int states) {
   int4* t = reinterpret_cast<int4*>(plan + tasks + static_cast<int64_t>(index) * kTaskWords);
   t[0] = make_int4(seq, len, rows, q);
   t[1] = make_int4(row, first, tiles, states);
-  for (int p = line.start(first) == at ? first : first + 1; p < line.n && line.start(p) < at + tiles; ++p)
+  for (int p = line.start(first) == at ? first : first + 1; p < first + states; ++p)
     *reinterpret_cast<int4*>(plan + pieces + static_cast<int64_t>(p) * kPieceWords) =
         make_int4(index, static_cast<int>(line.start(p) - at), static_cast<int>(line.start(p + 1) - line.start(p)), 0);
 }
 
 __device__ __forceinline__ int tiles_of(int len) { return static_cast<int>((static_cast<uint32_t>(len) + 31u) >> 5); }
 
+template <bool LDS>
 __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
-  __shared__ int64_t sums64[kWaves];
-  __shared__ int sums[kWaves];
+  constexpr int N = LDS ? kPlanLds + 1 : 1;
+  __shared__ int64_t sums[2][kWaves][2];
+  __shared__ int len_l[N], start_l[N], rank_l[N], list_l[N];
+  __shared__ int4 prompt_l[N];
+  __shared__ int2 where_l[N];
   const int tid = threadIdx.x, B = p.B, Nt = p.Nt, G = p.G;
   int32_t* plan = p.plan;
-  int32_t* qlist = plan + p.qlist;
-  int32_t* rank = plan + p.rank;
-  int4* prompts = reinterpret_cast<int4*>(plan + p.prompt);
+  int4* task1 = reinterpret_cast<int4*>(plan + p.task1);
+  Scan scan = {sums, 0};
+  auto len = [&](int s) { return LDS ? len_l[s] : p.seq_len[s]; };
+  auto start = [&](int b) { return LDS ? start_l[b] : p.q_start[b]; };
+  auto rank = [&](int i) -> int& { return LDS ? rank_l[i] : plan[p.rank + i]; };
+  auto list = [&](int k) { return LDS ? list_l[k] : plan[p.qlist + k]; };
+  auto prompt = [&](int b) -> int4& { return LDS ? prompt_l[b] : reinterpret_cast<int4*>(plan + p.prompt)[b]; };
 
   // checks; the active questions in order
   bool bad = false;
-  for (int b = tid; b < B; b += kThreads) {
-    const int qa = p.q_start[b], qb = p.q_start[b + 1];
-    bad = bad || qb < qa || qb - qa > p.max_questions || (b == 0 && qa != 0) || (b == B - 1 && qb != Nt);
+  for (int b = tid; b <= B; b += kThreads) {
+    const int qa = p.q_start[b], qb = b < B ? p.q_start[b + 1] : qa;
+    bad = bad || qb < qa || qb - qa > p.max_questions || (b == 0 && qa != 0) || (b == B && qa != Nt);
+    if constexpr (LDS) start_l[b] = qa;
   }
   for (int s = tid; s < B + Nt; s += kThreads) {
-    const int len = p.seq_len[s];
-    bad = bad || len < 0 || len > p.max_len;
+    const int n = p.seq_len[s];
+    bad = bad || n < 0 || n > p.max_len;
+    if constexpr (LDS) len_l[s] = n;
   }
+  int on0 = tid < Nt && p.active[tid] != 0;
   bad = __syncthreads_or(bad);
   int nact = 0;
   for (int i0 = 0; i0 < Nt; i0 += kThreads) {
     const int i = i0 + tid;
-    const int on = i < Nt && !bad && p.active[i] != 0;
+    const int on = !bad && (i0 == 0 ? on0 : i < Nt && p.active[i] != 0);
     int total;
-    const int ex = nact + block_exclusive<int>(on, sums, total);
-    if (i < Nt) rank[i] = ex;
-    if (on) qlist[ex] = i;
+    const int ex = nact + scan(on, total);
+    if (i < Nt) rank(i) = ex;
+    if (on) {
+      plan[p.qlist + ex] = i;
+      if constexpr (LDS) list_l[ex] = i;
+    }
     nact += total;
   }
-  if (tid == 0) rank[Nt] = nact;
+  if (tid == 0) rank(Nt) = nact;
   __syncthreads();
 
   // tiles of the two lines
-  int64_t t1 = 0, t2 = 0, w1 = 0;
+  int64_t t1 = 0, t2 = 0, T1, T2;
   if (!bad) {
     for (int b = tid; b < B; b += kThreads) {
-      const int n = rank[p.q_start[b + 1]] - rank[p.q_start[b]], tiles = tiles_of(p.seq_len[b]);
-      if (n == 0) continue;
-      if (p.group_q > 0 && n * G > 16) {
-        const int groups = (n + p.group_q - 1) / p.group_q;
-        t1 += static_cast<int64_t>(groups) * tiles;
-        w1 += static_cast<int64_t>(groups) * tiles;
-      } else {
-        t2 += tiles;
-      }
+      const int n = rank(start(b + 1)) - rank(start(b)), tiles = tiles_of(len(b));
+      if (p.group_q > 0 && n * G > 16) t1 += static_cast<int64_t>((n + p.group_q - 1) / p.group_q) * tiles;
+      else if (n > 0) t2 += tiles;
     }
-    for (int k = tid; k < nact; k += kThreads) t2 += tiles_of(p.seq_len[B + qlist[k]]);
+    for (int k = tid; k < nact; k += kThreads) t2 += tiles_of(len(B + list(k)));
   }
-  int64_t T1, T2, W1;
-  block_exclusive<int64_t>(t1, sums64, T1);
-  block_exclusive<int64_t>(t2, sums64, T2);
-  block_exclusive<int64_t>(w1, sums64, W1);
+  scan(t1, t2, T1, T2);
   // workgroups to the lines by their shares of the work, runs of four tiles
   // at least on the block line and of two on the wave line
   int n1 = 0, n2 = 0;
   if (T1 > 0) {
     const int64_t most = p.W - (T2 > 0 ? 1 : 0);
-    const int64_t share = (W1 * p.W + (W1 + T2) / 2) / (W1 + T2);
+    const int64_t share = quotient(T1 * p.W + (T1 + T2) / 2, T1 + T2);
     n1 = static_cast<int>(min(max(min(share, (T1 + 3) / 4), static_cast<int64_t>(1)), most));
   }
   if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(p.waves) * (p.W - n1), (T2 + 1) / 2));
   const Line line1(T1, n1), line2(T2, n2);
 
   // block line: contexts, their active questions in even groups
-  int tasks = 0, rows = 0;
-  int64_t at = 0;
+  int64_t tasks = 0, at = 0;
+  int rows = 0;
   for (int b0 = 0; b0 < B; b0 += kThreads) {
     const int b = b0 + tid;
-    int groups = 0, per = 0, n = 0, r0 = 0, len = 0, kind = 0;
+    int groups = 0, per = 0, n = 0, r0 = 0, tokens = 0, kind = 0;
     if (b < B && !bad) {
-      r0 = rank[p.q_start[b]];
-      n = rank[p.q_start[b + 1]] - r0;
-      len = p.seq_len[b];
-      if (n > 0 && len > 0) {
+      r0 = rank(start(b));
+      n = rank(start(b + 1)) - r0;
+      tokens = len(b);
+      if (n > 0 && tokens > 0) {
         kind = p.group_q > 0 && n * G > 16 ? 1 : 2;
         if (kind == 1) {
           groups = (n + p.group_q - 1) / p.group_q;
@@ -360,25 +426,27 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
         }
       }
     }
-    const int tiles = tiles_of(len);
-    int ntask;
-    const int task0 = tasks + block_exclusive<int>(groups, sums, ntask);
-    int64_t ntile;
-    const int64_t at0 = at + block_exclusive<int64_t>(static_cast<int64_t>(groups) * tiles, sums64, ntile);
+    const int tiles = tiles_of(tokens);
+    int64_t task0 = groups, at0 = static_cast<int64_t>(groups) * tiles, ntask, ntile;
+    scan(task0, at0, ntask, ntile);
+    task0 += tasks;
+    at0 += at;
     int need = 0;
     for (int j = 0; j < groups; ++j) {
       const int64_t x = at0 + static_cast<int64_t>(j) * tiles;
       need += (line1.piece_of(x + tiles - 1) - line1.piece_of(x) + 1) * (min(per, n - j * per) * G);
     }
     int nrow;
-    int row = rows + block_exclusive<int>(need, sums, nrow);
+    int row = rows + scan(need, nrow);
     for (int j = 0; j < groups; ++j) {
       const int64_t x = at0 + static_cast<int64_t>(j) * tiles;
-      const int gr = min(per, n - j * per) * G, states = line1.piece_of(x + tiles - 1) - line1.piece_of(x) + 1;
-      write_task(plan, p.task1, p.piece1, line1, task0 + j, x, tiles, b, len, gr, r0 + j * per, row, states);
+      const int gr = min(per, n - j * per) * G, first = line1.piece_of(x), states = line1.piece_of(x + tiles - 1) - first + 1;
+      const int t = static_cast<int>(task0) + j;
+      write_task(plan, p.task1, p.piece1, line1, t, x, tiles, b, tokens, gr, r0 + j * per, row, first, states);
+      if constexpr (LDS) where_l[t] = make_int2(row, states);
       row += states * gr;
     }
-    if (b < B) prompts[b] = make_int4(kind, task0, per, r0);
+    if (b < B) prompt(b) = make_int4(kind, static_cast<int>(task0), per, r0);
     tasks += ntask;
     rows += nrow;
     at += ntile;
@@ -386,36 +454,39 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __syncthreads();                                   // prompts
 
   // wave line: the other contexts, then the segments of the active questions
-  tasks = 0;
-  at = 0;
+  tasks = at = 0;
   for (int x0 = 0; x0 < B + nact; x0 += kThreads) {
     const int x = x0 + tid;
-    int seq = -1, len = 0, q = 0, n = 0;
+    int seq = -1, tokens = 0, q = 0, n = 0;
     if (x < B) {
-      const int4 pr = prompts[x];
+      const int4 pr = prompt(x);
       if (pr.x == 2) {
         seq = x;
         q = pr.w;
-        n = (rank[p.q_start[x + 1]] - q) * G;
-        len = p.seq_len[x];
+        n = (rank(start(x + 1)) - q) * G;
+        tokens = len(x);
       }
     } else if (x < B + nact) {
       q = x - B;
-      seq = B + qlist[q];
+      seq = B + list(q);
       n = G;
-      len = p.seq_len[seq];
+      tokens = len(seq);
     }
-    const int tiles = seq < 0 ? 0 : tiles_of(len);
-    int ntask;
-    const int task = tasks + block_exclusive<int>(tiles > 0, sums, ntask);
-    int64_t ntile;
-    const int64_t at0 = at + block_exclusive<int64_t>(tiles, sums64, ntile);
-    const int np = tiles > 0 ? line2.piece_of(at0 + tiles - 1) - line2.piece_of(at0) + 1 : 0;
+    const int tiles = tiles_of(tokens);
+    int64_t task = tiles > 0, at0 = tiles, ntask, ntile;
+    scan(task, at0, ntask, ntile);
+    task += tasks;
+    at0 += at;
+    const int first = tiles > 0 ? line2.piece_of(at0) : 0, np = tiles > 0 ? line2.piece_of(at0 + tiles - 1) - first + 1 : 0;
     int nrow;
-    const int row = rows + block_exclusive<int>(np * n, sums, nrow);
-    if (tiles > 0) write_task(plan, p.task2, p.piece2, line2, task, at0, tiles, seq, len, n, q, row, np);
+    const int row = rows + scan(np * n, nrow);
+    if (tiles > 0)
+      write_task(plan, p.task2, p.piece2, line2, static_cast<int>(task), at0, tiles, seq, tokens, n, q, row, first, np);
     if (x < B) {
-      if (seq >= 0) prompts[x].y = task;
+      if (seq >= 0) {
+        prompt(x).y = row;
+        prompt(x).z = np;
+      }
     } else if (x < B + nact) {
       *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(seq - B) * kQuestionWords + 4) = make_int4(row, np, 0, 0);
     }
@@ -423,30 +494,40 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     rows += nrow;
     at += ntile;
   }
-  __syncthreads();                                   // tasks of contexts
+  __syncthreads();                                   // states of contexts
 
   // where the states of each question's context are
   for (int i = tid; i < Nt; i += kThreads) {
-    const int k = rank[i];
+    const int k = rank(i);
     int4 rec = make_int4(0, 0, 0, 0);
-    if (rank[i + 1] > k) {
-      const int b = last_at_most(p.q_start, B, i);
-      const int4 pr = prompts[b];
+    if (rank(i + 1) > k) {
+      int lo = 0, hi = B - 1;                        // the last prompt that starts at i at most
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start(mid) <= i) lo = mid; else hi = mid - 1;
+      }
+      const int4 pr = prompt(lo);
       rec.x = 1;
-      if (pr.x != 0) {
-        const int local = k - pr.w, j = pr.x == 1 ? local / pr.z : 0;
-        const int64_t rec0 = (pr.x == 1 ? p.task1 : p.task2) + static_cast<int64_t>(pr.y + j) * kTaskWords;
-        const int4 ta = reinterpret_cast<const int4*>(plan + rec0)[0], tb = reinterpret_cast<const int4*>(plan + rec0)[1];
-        rec.y = tb.x + (local - j * (pr.x == 1 ? pr.z : 0)) * G;
+      if (pr.x == 1) {                               // (first task, questions a group)
+        const int local = k - pr.w, j = local / pr.z;
+        const int4 tb = LDS ? make_int4(where_l[pr.y + j].x, 0, 0, where_l[pr.y + j].y) : task1[2 * (pr.y + j) + 1];
+        rec.y = tb.x + (local - j * pr.z) * G;
         rec.z = tb.w;
-        rec.w = ta.z;
+        rec.w = min(pr.z, rank(start(lo + 1)) - pr.w - j * pr.z) * G;
+      } else if (pr.x == 2) {                        // (first state's row, states)
+        rec.y = pr.y + (k - pr.w) * G;
+        rec.z = pr.z;
+        rec.w = (rank(start(lo + 1)) - pr.w) * G;
       }
     }
     *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(i) * kQuestionWords) = rec;
   }
   if (tid < kPlanHeader) {
     const int head[9] = {kPlanMagic, B, Nt, p.W, p.group_q, G, n1, n2, p.max_len};
-    plan[tid] = tid < 9 ? head[tid] : 0;
+    int word = 0;
+#pragma unroll
+    for (int w = 0; w < 9; ++w) word = tid == w ? head[w] : word;
+    plan[tid] = word;
   }
   if (bad && tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
@@ -466,7 +547,8 @@ hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s) {
 }
 
 hipError_t launch_paged_plan(const PagedPlanParams& p, hipStream_t s) {
-  plan_kernel<<<1, kThreads, 0, s>>>(p);
+  if (p.B + p.Nt <= kPlanLds) plan_kernel<true><<<1, kThreads, 0, s>>>(p);
+  else plan_kernel<false><<<1, kThreads, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -22,6 +22,9 @@ import torch
 from . import _lib as L
 from .session import torch_dtype
 
+# the current stream's handle without a Stream object around it (0.1 against 1.1 us)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
 
 class PagedBatch:
     """Prompts with ``q_count`` questions each on one GPU; sequences 0..B-1 are their
@@ -44,6 +47,7 @@ class PagedBatch:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else None
         self.dtype = dtype
         self.tdtype = torch_dtype(dtype)
         self.q_count = np.asarray(q_count, dtype=np.int64)
@@ -113,22 +117,32 @@ class PagedBatch:
         self.ws = torch.empty(max(self.ws_bytes, 256), dtype=torch.uint8, device=dev)
 
     # ------------------------------------------------------------------ helpers
-    def _expect(self, t: torch.Tensor, name: str, shape, dtype, contiguous: bool = True) -> None:
-        if t.device != self.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
-                (contiguous and not t.is_contiguous()):
-            raise ValueError(f"{name}: {dtype} {tuple(shape)} on {self.device}" + (", contiguous" if contiguous else ""))
+    # A decode step makes a few calls a layer of some microseconds each, so the
+    # checks below are a handful of attribute reads per tensor.
+    def _expect(self, t: torch.Tensor, name: str, shape, dtype) -> int:
+        """The address of a contiguous tensor of this shape and type on the batch's device."""
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: {dtype} {tuple(shape)} on {self.device}, contiguous")
+        return t.data_ptr()
 
-    def _rows(self, t: torch.Tensor, name: str, rows: int, heads: int) -> int:
+    def _row_stride(self, t: torch.Tensor, name: str, rows: int, heads: int) -> int:
         """Elements between the rows of [rows, heads * D] or [rows, heads, D], whose heads lie together."""
-        inner = tuple(t.shape[1:])
-        flat = inner == (heads * self.D,) and t.stride(1) == 1
-        split = inner == (heads, self.D) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == self.D)
-        if t.device != self.device or t.dtype != self.tdtype or t.shape[0] != rows or not (flat or split):
+        shape, stride = t.shape, t.stride()
+        flat = shape == (rows, heads * self.D) and stride[1] == 1
+        if t.dtype is not self.tdtype or t.device != self.device or not (
+                flat or (shape == (rows, heads, self.D) and stride[2] == 1 and (heads == 1 or stride[1] == self.D))):
             raise ValueError(f"{name}: {self.tdtype} [{rows}, {heads}, {self.D}] on {self.device}, a row's elements together")
-        return t.stride(0) if rows > 1 else heads * self.D
+        return stride[0] if rows > 1 else heads * self.D
 
-    def stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+    def _call(self, fn, *args) -> None:
+        """fn(batch, *args, current stream of the batch's device), with that device the current one."""
+        if self._index is None:
+            raise ValueError("the batch's buffers are not on a GPU")
+        if torch.cuda.current_device() == self._index:
+            fn(self.batch, *args, _raw_stream(self._index))
+        else:
+            with torch.cuda.device(self._index):
+                fn(self.batch, *args, _raw_stream(self._index))
 
     def err_flag(self) -> int:
         return int(self.err.item())
@@ -142,49 +156,37 @@ class PagedBatch:
                 positions: torch.Tensor, served: torch.Tensor) -> None:
         """Lengths, tables and slots of a change of the sequences: see ippd_paged_reserve."""
         n, i32 = self.B + self.Nt, torch.int32
-        self._expect(new_tokens, "new_tokens", (n,), i32)
-        self._expect(token_start, "token_start", (n + 1,), i32)
-        self._expect(slot_map, "slot_map", (num_rows,), i32)
-        self._expect(positions, "positions", (num_rows,), i32)
-        self._expect(served, "served", (n,), i32)
-        with torch.cuda.device(self.device):
-            L.ippd_paged_reserve(self.batch, new_tokens.data_ptr(), token_start.data_ptr(), num_rows,
-                                 slot_map.data_ptr(), positions.data_ptr(), served.data_ptr(), self.stream())
+        self._call(L.ippd_paged_reserve, self._expect(new_tokens, "new_tokens", (n,), i32),
+                   self._expect(token_start, "token_start", (n + 1,), i32), num_rows,
+                   self._expect(slot_map, "slot_map", (num_rows,), i32),
+                   self._expect(positions, "positions", (num_rows,), i32), self._expect(served, "served", (n,), i32))
 
     def append(self, layer: int, slot_map: torch.Tensor, positions: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                q: Optional[torch.Tensor] = None, q_rot: Optional[torch.Tensor] = None) -> None:
         """Rotate the rows' tokens and write them into a layer's pages; with q, its rotation into q_rot."""
         rows = slot_map.shape[0]
-        self._expect(slot_map, "slot_map", (rows,), torch.int32)
-        self._expect(positions, "positions", (rows,), torch.int32)
-        if rows == 0:
-            return
-        ks, vs = self._rows(k, "k", rows, self.hkv), self._rows(v, "v", rows, self.hkv)
+        sm = self._expect(slot_map, "slot_map", (rows,), torch.int32)
+        ps = self._expect(positions, "positions", (rows,), torch.int32)
+        ks, vs = self._row_stride(k, "k", rows, self.hkv), self._row_stride(v, "v", rows, self.hkv)
         qs, qp, qr = 0, None, None
         if q is not None:
-            qs, qp = self._rows(q, "q", rows, self.hq), q.data_ptr()
             if q_rot is None:
                 raise ValueError("q needs q_rot")
-            self._expect(q_rot, "q_rot", (rows, self.hq, self.D), self.tdtype)
-            qr = q_rot.data_ptr()
-        with torch.cuda.device(self.device):
-            L.ippd_paged_append(self.batch, self.pages[layer], rows, slot_map.data_ptr(), positions.data_ptr(), qp, qs,
-                                k.data_ptr(), ks, v.data_ptr(), vs, qr, self.stream())
+            qs, qp = self._row_stride(q, "q", rows, self.hq), q.data_ptr()
+            qr = self._expect(q_rot, "q_rot", (rows, self.hq, self.D), self.tdtype)
+        if rows:
+            self._call(L.ippd_paged_append, self.pages[layer], rows, sm, ps, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, qr)
 
     def plan(self) -> None:
         """Plan this step's attention from the lengths and active flags (once for all layers)."""
-        with torch.cuda.device(self.device):
-            L.ippd_paged_plan(self.batch, self.plan_buf.data_ptr(), self.plan_bytes, self.stream())
+        self._call(L.ippd_paged_plan, self.plan_buf.data_ptr(), self.plan_bytes)
 
     def decode(self, layer: int, q_rot: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
         """The planned step's attention over a layer's pages: q_rot, out [Nt, Hq, D], lse float32 [Nt, Hq]."""
         if self.Nt == 0:
             return
-        self._expect(q_rot, "q_rot", (self.Nt, self.hq, self.D), self.tdtype)
-        self._expect(out, "out", (self.Nt, self.hq, self.D), self.tdtype)
-        if lse is not None:
-            self._expect(lse, "lse", (self.Nt, self.hq), torch.float32)
-        with torch.cuda.device(self.device):
-            L.ippd_paged_decode_attention(self.batch, self.pages[layer], self.plan_buf.data_ptr(), self.plan_bytes,
-                                          q_rot.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
-                                          self.ws.data_ptr(), self.ws_bytes, self.stream())
+        shape = (self.Nt, self.hq, self.D)
+        qp, op = self._expect(q_rot, "q_rot", shape, self.tdtype), self._expect(out, "out", shape, self.tdtype)
+        lp = None if lse is None else self._expect(lse, "lse", shape[:2], torch.float32)
+        self._call(L.ippd_paged_decode_attention, self.pages[layer], self.plan_buf.data_ptr(), self.plan_bytes, qp, op,
+                   lp, self.ws.data_ptr(), self.ws_bytes)
