@@ -12,7 +12,7 @@ namespace ippd {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 1024;                       // at most; a launch has as many as its sequences (or rows) ask for
 constexpr int kWaves = kThreads / 64;
 // reserve_kernel fills the slot map itself up to these sizes (one launch); its
 // copies of the sequences' rows and lengths then fit the LDS
@@ -65,6 +65,10 @@ __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
 struct Scan {
   int64_t (*lds)[kWaves][2];
   int turn;
+  // The places of waves that the launch does not have; a barrier follows.
+  __device__ __forceinline__ void clear() const {
+    if (threadIdx.x < 4 * kWaves) (&lds[0][0][0])[threadIdx.x] = 0;
+  }
   template <typename V>
   __device__ __forceinline__ V place(V inc, int col, int64_t (*at)[2], V& total) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -147,34 +151,36 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
   __shared__ int taken;
   __shared__ int row0[ROWS ? kFusedSequences : 1], after[ROWS ? kFusedSequences : 1], got[ROWS ? kFusedSequences : 1];
   __shared__ int q0[ROWS ? kFusedSequences : 1];
-  const int tid = threadIdx.x, S = p.B + p.Nt, sh = p.page_shift;
+  const int tid = threadIdx.x, threads = blockDim.x, S = p.B + p.Nt, sh = p.page_shift;
   const int64_t cap = static_cast<int64_t>(p.table_pages) << sh;
   const int f = *p.free_count;
   Scan scan = {sums, 0};
+  scan.clear();
   if (tid == 0) taken = 0;
 
   // checks, and the pages given back
   bool bad = f < 0 || f > p.num_pages;
   int64_t back = 0;
-  for (int s = tid; s < S; s += kThreads) {
+  for (int s = tid; s < S; s += threads) {
     const int len = p.seq_len[s], c = p.new_tokens[s], a = p.token_start[s], e = p.token_start[s + 1];
     bad = bad || len < 0 || len > cap || a < 0 || e < a || e > p.num_rows || c > e - a;
     if (c < 0 && len > 0) back += pages_of(len, sh) - pages_of(c < -len ? 0 : len + c, sh);
     if constexpr (ROWS) row0[s] = a;
   }
-  for (int b = tid; b < p.B; b += kThreads) {
+  for (int b = tid; b < p.B; b += threads) {
     const int qa = p.q_start[b], qb = p.q_start[b + 1];
     bad = bad || qb < qa || (b == 0 && qa != 0) || (b == p.B - 1 && qb != p.Nt);
     if constexpr (ROWS) q0[b] = qa;
   }
+  __syncthreads();
   int64_t total_back, none = 0, zero;
   scan(back, none, total_back, zero);
   bad = __syncthreads_or(bad || total_back > p.num_pages - f);
   if (bad) {                                         // nothing is moved: no row of the call is served
     if (tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
-    for (int s = tid; s < S; s += kThreads) p.served[s] = 0;
+    for (int s = tid; s < S; s += threads) p.served[s] = 0;
     if constexpr (ROWS) {
-      for (int r = tid; r < p.num_rows; r += kThreads) {
+      for (int r = tid; r < p.num_rows; r += threads) {
         p.slot_map[r] = -1;
         p.positions[r] = -1;
       }
@@ -186,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
   // shrink
   if (R > 0) {
     int carry = 0;
-    for (int s0 = 0; s0 < S; s0 += kThreads) {
+    for (int s0 = 0; s0 < S; s0 += threads) {
       const int s = s0 + tid;
       int n = 0, keep = 0;
       if (s < S) {
@@ -201,8 +207,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
       first[tid] = ex;
       from[tid] = keep;
       __syncthreads();
-      for (int k = tid; k < total; k += kThreads) {
-        const int w = last_at_most(first, min(kThreads, S - s0), k);
+      for (int k = tid; k < total; k += threads) {
+        const int w = last_at_most(first, min(threads, S - s0), k);
         const int64_t row = static_cast<int64_t>(s0 + w) * p.table_pages;
         p.free_pages[f1 - 1 - (carry + k)] = p.block_table[row + from[w] + (k - first[w])];
       }
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
 
   // grow
   int carry = 0;
-  for (int s0 = 0; s0 < S; s0 += kThreads) {
+  for (int s0 = 0; s0 < S; s0 += threads) {
     const int s = s0 + tid;
     int need = 0, len = 0, c = 0, have = 0;
     bool fits = false;
@@ -260,8 +266,8 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
     __syncthreads();
     // the served sequences are those of a leading run of the pages needed
     const int run = min(total, taken - carry);
-    for (int k = tid; k < run; k += kThreads) {
-      const int w = last_at_most(first, min(kThreads, S - s0), k);
+    for (int k = tid; k < run; k += threads) {
+      const int w = last_at_most(first, min(threads, S - s0), k);
       const int64_t row = static_cast<int64_t>(s0 + w) * p.table_pages;
       p.block_table[row + from[w] + (k - first[w])] = p.free_pages[f1 - 1 - (carry + k)];
     }
@@ -270,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
   __syncthreads();                                   // tables, and the page count
   if (tid == 0) *p.free_count = f1 - taken;
   if constexpr (ROWS) {
-    for (int r = tid; r < p.num_rows; r += kThreads) {
+    for (int r = tid; r < p.num_rows; r += threads) {
       const int s = last_at_most(row0, S, r);
       int base = 0;
       if (s >= p.B) base = after[last_at_most(q0, p.B, s - p.B)];
@@ -346,10 +352,11 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __shared__ int len_l[N], start_l[N], rank_l[N], list_l[N];
   __shared__ int4 prompt_l[N];
   __shared__ int2 where_l[N];
-  const int tid = threadIdx.x, B = p.B, Nt = p.Nt, G = p.G;
+  const int tid = threadIdx.x, threads = blockDim.x, B = p.B, Nt = p.Nt, G = p.G;
   int32_t* plan = p.plan;
   int4* task1 = reinterpret_cast<int4*>(plan + p.task1);
   Scan scan = {sums, 0};
+  scan.clear();
   auto len = [&](int s) { return LDS ? len_l[s] : p.seq_len[s]; };
   auto start = [&](int b) { return LDS ? start_l[b] : p.q_start[b]; };
   auto rank = [&](int i) -> int& { return LDS ? rank_l[i] : plan[p.rank + i]; };
@@ -358,12 +365,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
 
   // checks; the active questions in order
   bool bad = false;
-  for (int b = tid; b <= B; b += kThreads) {
+  for (int b = tid; b <= B; b += threads) {
     const int qa = p.q_start[b], qb = b < B ? p.q_start[b + 1] : qa;
     bad = bad || qb < qa || qb - qa > p.max_questions || (b == 0 && qa != 0) || (b == B && qa != Nt);
     if constexpr (LDS) start_l[b] = qa;
   }
-  for (int s = tid; s < B + Nt; s += kThreads) {
+  for (int s = tid; s < B + Nt; s += threads) {
     const int n = p.seq_len[s];
     bad = bad || n < 0 || n > p.max_len;
     if constexpr (LDS) len_l[s] = n;
@@ -371,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   int on0 = tid < Nt && p.active[tid] != 0;
   bad = __syncthreads_or(bad);
   int nact = 0;
-  for (int i0 = 0; i0 < Nt; i0 += kThreads) {
+  for (int i0 = 0; i0 < Nt; i0 += threads) {
     const int i = i0 + tid;
     const int on = !bad && (i0 == 0 ? on0 : i < Nt && p.active[i] != 0);
     int total;
@@ -389,12 +396,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   // tiles of the two lines
   int64_t t1 = 0, t2 = 0, T1, T2;
   if (!bad) {
-    for (int b = tid; b < B; b += kThreads) {
+    for (int b = tid; b < B; b += threads) {
       const int n = rank(start(b + 1)) - rank(start(b)), tiles = tiles_of(len(b));
       if (p.group_q > 0 && n * G > 16) t1 += static_cast<int64_t>((n + p.group_q - 1) / p.group_q) * tiles;
       else if (n > 0) t2 += tiles;
     }
-    for (int k = tid; k < nact; k += kThreads) t2 += tiles_of(len(B + list(k)));
+    for (int k = tid; k < nact; k += threads) t2 += tiles_of(len(B + list(k)));
   }
   scan(t1, t2, T1, T2);
   // workgroups to the lines by their shares of the work, runs of four tiles
@@ -411,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   // block line: contexts, their active questions in even groups
   int64_t tasks = 0, at = 0;
   int rows = 0;
-  for (int b0 = 0; b0 < B; b0 += kThreads) {
+  for (int b0 = 0; b0 < B; b0 += threads) {
     const int b = b0 + tid;
     int groups = 0, per = 0, n = 0, r0 = 0, tokens = 0, kind = 0;
     if (b < B && !bad) {
@@ -455,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
 
   // wave line: the other contexts, then the segments of the active questions
   tasks = at = 0;
-  for (int x0 = 0; x0 < B + nact; x0 += kThreads) {
+  for (int x0 = 0; x0 < B + nact; x0 += threads) {
     const int x = x0 + tid;
     int seq = -1, tokens = 0, q = 0, n = 0;
     if (x < B) {
@@ -497,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __syncthreads();                                   // states of contexts
 
   // where the states of each question's context are
-  for (int i = tid; i < Nt; i += kThreads) {
+  for (int i = tid; i < Nt; i += threads) {
     const int k = rank(i);
     int4 rec = make_int4(0, 0, 0, 0);
     if (rank(i + 1) > k) {
@@ -522,21 +529,26 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     }
     *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(i) * kQuestionWords) = rec;
   }
-  if (tid < kPlanHeader) {
-    const int head[9] = {kPlanMagic, B, Nt, p.W, p.group_q, G, n1, n2, p.max_len};
-    int word = 0;
-#pragma unroll
-    for (int w = 0; w < 9; ++w) word = tid == w ? head[w] : word;
-    plan[tid] = word;
+  if (tid == 0) {
+    int4* head = reinterpret_cast<int4*>(plan);
+    head[0] = make_int4(kPlanMagic, B, Nt, p.W);
+    head[1] = make_int4(p.group_q, G, n1, n2);
+    head[2] = make_int4(p.max_len, 0, 0, 0);
   }
   if (bad && tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
 
 }  // namespace
 
+// Threads for n items: whole waves, kThreads at most.  These kernels are bound
+// by latency and, where waves share a SIMD, by the instructions of all of them,
+// so that idle waves cost: plan of 264 sequences 10.5 us with 1024 threads.
+static int threads_for(int64_t n) { return static_cast<int>(n >= kThreads ? kThreads : n <= 64 ? 64 : (n + 63) / 64 * 64); }
+
 hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s) {
-  if (p.num_rows <= kFusedRows && p.B + p.Nt <= kFusedSequences) {
-    reserve_kernel<true><<<1, kThreads, 0, s>>>(p);
+  const int sequences = p.B + p.Nt;
+  if (p.num_rows <= kFusedRows && sequences <= kFusedSequences) {
+    reserve_kernel<true><<<1, threads_for(sequences > p.num_rows ? sequences : p.num_rows), 0, s>>>(p);
     return hipGetLastError();
   }
   reserve_kernel<false><<<1, kThreads, 0, s>>>(p);
@@ -547,8 +559,9 @@ hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s) {
 }
 
 hipError_t launch_paged_plan(const PagedPlanParams& p, hipStream_t s) {
-  if (p.B + p.Nt <= kPlanLds) plan_kernel<true><<<1, kThreads, 0, s>>>(p);
-  else plan_kernel<false><<<1, kThreads, 0, s>>>(p);
+  const int sequences = p.B + p.Nt, threads = threads_for(sequences);
+  if (sequences <= kPlanLds) plan_kernel<true><<<1, threads, 0, s>>>(p);
+  else plan_kernel<false><<<1, threads, 0, s>>>(p);
   return hipGetLastError();
 }
 
