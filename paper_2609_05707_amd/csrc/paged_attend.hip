@@ -11,6 +11,8 @@
 // read through the scalar cache a tile ahead, apart from the vector loads that
 // carry keys and values; an id outside the pool marks the piece's states as
 // bad (l = -1), its tiles are read from page 0, and the question gets no output.
+#include <algorithm>
+
 #include "ippd_device.h"
 #include "paged_internal.h"
 #include "tile_attend.h"
@@ -354,79 +356,150 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
 }
 
 // ---------------------------------------------------------------------------
-// Wave line: a wave streams its piece's tiles through its registers, the next
-// tile's keys and values in flight while it computes.
+// Wave line: a wave streams its piece's tiles through its registers.  The next
+// tile's keys and values are in flight while it computes one, across the ends
+// of tasks too (a short segment is a tile or two): the page ids run two tiles
+// ahead, the record of the next task a task ahead, all by scalar loads.  Loads
+// of a last tile stay within the sequence's tokens, so that a segment costs the
+// bytes it has.
 // ---------------------------------------------------------------------------
+// A tile of a piece: its task and the tile within it.
+struct Place {
+  Task task;
+  int index, tile;
+};
+
+template <bool SMALL>
+__device__ __forceinline__ int2 page_ids(const PagedAttendParams& p, const Place& at) {
+  scalar_words table = scalars(p.block_table + static_cast<int64_t>(at.task.seq) * p.table_pages);
+  const int shift = SMALL ? 4 : p.page_shift, a = (at.tile << 5) >> shift, last = (at.task.len - 1) >> shift;
+  const int x = table[min(a, last)];
+  return make_int2(x, SMALL ? table[min(a + 1, last)] : x);
+}
+
 template <typename T, int D, bool SMALL>
 __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece, int g, int lane) {
   using M = Mfma<T>;
   const int lr = lane & 15, lg = lane >> 4;
   scalar_words pw = scalars(p.plan + p.piece2 + static_cast<int64_t>(piece) * kPieceWords);
-  int index = pw[0], tile = pw[1], left = pw[2];
-  // this lane's elements of a tile: keys of tokens tile_token(kb, lr), values of
-  // the 8 tokens of block lg; at 16 tokens a page the second page's start over
-  const int ktok = tile_token(0, lr), vtok = 8 * lg;
-  const bool k2 = SMALL && ktok >= 16, v2 = SMALL && vtok >= 16;
-  const int koff = (k2 ? ktok - 16 : ktok) * D + 8 * lg, voff = (v2 ? vtok - 16 : vtok) * D + 8 * lr;
-  while (left > 0) {
-    Task task;
-    task.load(p.plan, p.task2 + static_cast<int64_t>(index) * kTaskWords);
-    const int n = min(left, task.tiles - tile);
-    Pages<SMALL> pages;
-    pages.init(p, task.seq, task.len);
-    typename M::Frag qf[D / 32], kf[2][D / 32], vf[D / 16];
-    auto load_keys = [&](int2 id, int t) {
-      const int64_t a = page_at<SMALL, D>(p, id.x, g, t), b = SMALL ? page_at<SMALL, D>(p, id.y, g, t) : a;
-      const T* src = static_cast<const T*>(p.k_pages) + (k2 ? b : a) + koff;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int ds = 0; ds < D / 32; ++ds) kf[kb][ds] = M::load(src + 4 * kb * D + 32 * ds);
-    };
-    auto load_values = [&](int2 id, int t) {
-      const int64_t a = page_at<SMALL, D>(p, id.x, g, t), b = SMALL ? page_at<SMALL, D>(p, id.y, g, t) : a;
-      const T* src = static_cast<const T*>(p.v_pages) + (v2 ? b : a) + voff;
-#pragma unroll
-      for (int db = 0; db < D / 16; ++db) vf[db] = M::load(src + 128 * db);
-    };
-    int2 id = pages.checked(pages.of(tile));
-    load_query<T, D>(p, qf, task.q, min(lr, task.rows - 1), g, lg);
-    load_keys(id, tile);
-    load_values(id, tile);
-    int2 next = pages.of(min(tile + 1, task.tiles - 1));
-    State<D> st;
-    clear(st);
-    for (int t = 0; t < n; ++t) {
-      id = pages.checked(next);
-      next = pages.of(min(tile + t + 2, task.tiles - 1));
-      const int nt = min(tile + t + 1, task.tiles - 1);
-      f32x4_t sc[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        sc[kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ds = 0; ds < D / 32; ++ds) sc[kb] = M::mma(kf[kb][ds], qf[ds], sc[kb]);
-      }
-      if (t + 1 < n) load_keys(id, nt);
-      const int m = task.len - 32 * (tile + t);
-      if (m < 32) mask_scores(sc, m, lg);
-      const typename M::Frag pf = fold<T, D>(sc, st, p.c);
-      if (m < 32) {                                  // what lies past the end may be anything
-        const int keep = min(max(m - 8 * lg, 0), 8);
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) vf[db] = M::keep_first(vf[db], keep);
-      }
-#pragma unroll
-      for (int db = 0; db < D / 16; ++db) st.o[db] = M::mma(vf[db], pf, st.o[db]);
-      if (t + 1 < n) load_values(id, nt);
+  const int n = pw[2];
+  Place now, next, far;                              // computed, loaded, page ids read
+  Task after;                                        // the task behind far's
+  now.index = pw[0];
+  now.tile = pw[1];
+  now.task.load(p.plan, p.task2 + static_cast<int64_t>(now.index) * kTaskWords);
+  after.load(p.plan, p.task2 + static_cast<int64_t>(now.index + 1) * kTaskWords);
+  // (the record behind a line's last task is within the plan, and not used)
+  auto advance = [&](Place& at) {
+    if (++at.tile < at.task.tiles) return;
+    at.task = after;
+    at.tile = 0;
+    ++at.index;
+    after.load(p.plan, p.task2 + static_cast<int64_t>(at.index + 1) * kTaskWords);
+  };
+  // the place of tile t, or, behind the piece's last, that one again
+  auto follow = [&](Place& at, int t) {
+    if (t < n) advance(at);
+  };
+  auto checked = [&](int2 id, bool& no) {
+    no = static_cast<uint32_t>(id.x) >= static_cast<uint32_t>(p.num_pages) ||
+         (SMALL && static_cast<uint32_t>(id.y) >= static_cast<uint32_t>(p.num_pages));
+    return no ? make_int2(0, 0) : id;
+  };
+  // this lane's keys of a tile are those of tokens tile_token(kb, lr), its values
+  // those of the eight tokens of block lg; at 16 tokens a page tokens 16 .. 31
+  // are the second page's
+  const int ktok = tile_token(0, lr);
+  auto base_of = [&](const void* pages, int2 id, int tile, int& tok) {
+    int64_t at = page_at<SMALL, D>(p, id.x, g, tile);
+    if (SMALL && tok >= 16) {
+      at = page_at<SMALL, D>(p, id.y, g, tile);
+      tok -= 16;
     }
-    if (pages.bad && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
-    const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
-    publish<D>(p, st, row + lr, lr < task.rows, pages.bad, lg);
-    left -= n;
-    tile = 0;
-    ++index;
+    return static_cast<const T*>(pages) + at;
+  };
+  typename M::Frag qf[D / 32], qn[D / 32], kf[2][D / 32], vf[D / 16];
+  auto load_keys = [&](const Place& at, int2 id) {
+    const int lim = at.task.len - 1 - 32 * at.tile;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      int tok = min(ktok + 4 * kb, lim);
+      const T* src = base_of(p.k_pages, id, at.tile, tok) + tok * D + 8 * lg;
+#pragma unroll
+      for (int ds = 0; ds < D / 32; ++ds) kf[kb][ds] = M::load(src + 32 * ds);
+    }
+  };
+  auto load_values = [&](const Place& at, int2 id) {
+    int tok = 8 * min(lg, (at.task.len - 1 - 32 * at.tile) >> 3);
+    const T* src = base_of(p.v_pages, id, at.tile, tok) + tok * D + 8 * lr;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) vf[db] = M::load(src + 128 * db);
+  };
+  auto load_rows = [&](const Task& task, typename M::Frag (&f)[D / 32]) {
+    const int r = min(lr, task.rows - 1);
+    int i = task.seq - p.B, h = r;                   // a segment's rows are its question's heads
+    if (task.seq < p.B) {
+      i = p.plan[p.qlist + task.q + r / p.G];
+      h = r % p.G;
+    }
+    const T* src = static_cast<const T*>(p.q_rot) + (static_cast<int64_t>(i) * p.Hq + g * p.G + h) * D + 8 * lg;
+#pragma unroll
+    for (int ds = 0; ds < D / 32; ++ds) f[ds] = M::load(src + 32 * ds);
+  };
+  int2 id = page_ids<SMALL>(p, now);
+  far = now;
+  follow(far, 1);
+  int2 ahead = page_ids<SMALL>(p, far);
+  load_rows(now.task, qf);
+  bool bad, bad_next;                                // of the task computed; of the tile loaded
+  id = checked(id, bad);
+  bool any = bad;
+  load_keys(now, id);
+  load_values(now, id);
+  next = far;
+  State<D> st;
+  clear(st);
+  for (int t = 0; t < n; ++t) {
+    const bool ends = t + 1 >= n || next.index != now.index;   // the last tile of its task here
+    const bool more = t + 1 < n;
+    id = checked(ahead, bad_next);
+    any = any || bad_next;
+    follow(far, t + 2);
+    ahead = page_ids<SMALL>(p, far);
+    if (more && ends) load_rows(next.task, qn);
+    f32x4_t sc[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      sc[kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ds = 0; ds < D / 32; ++ds) sc[kb] = M::mma(kf[kb][ds], qf[ds], sc[kb]);
+    }
+    if (more) load_keys(next, id);
+    const int m = now.task.len - 32 * now.tile;
+    if (m < 32) mask_scores(sc, m, lg);
+    const typename M::Frag pf = fold<T, D>(sc, st, p.c);
+    if (m < 32) {                                    // what lies past the end may be anything
+      const int keep = min(max(m - 8 * lg, 0), 8);
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) vf[db] = M::keep_first(vf[db], keep);
+    }
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) st.o[db] = M::mma(vf[db], pf, st.o[db]);
+    if (more) load_values(next, id);
+    if (ends) {
+      const int64_t row = static_cast<int64_t>(g) * p.rows + now.task.row +
+                          static_cast<int64_t>(piece - now.task.first) * now.task.rows;
+      publish<D>(p, st, row + lr, lr < now.task.rows, bad, lg);
+      bad = false;
+      clear(st);
+#pragma unroll
+      for (int ds = 0; ds < D / 32; ++ds) qf[ds] = qn[ds];
+    }
+    bad = bad || bad_next;
+    now = next;
+    next = far;
   }
+  if (any && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
 
 // Whether the buffer holds a plan of this batch's sizes.
@@ -455,10 +528,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendPar
 }
 
 // ---------------------------------------------------------------------------
-// Join: a workgroup per (question, kv head).  An item is four dims of one head;
-// as many threads as there are share an item's states and are joined in LDS.
+// Join: a unit of one, two or four waves takes a (question, head).  A lane folds
+// every (64 / (D / 4) x waves)-th of the head's states for four dims; lanes of a
+// wave are joined by swaps, waves in LDS.  The plan says how many states the
+// widest question has, and with it how many waves a unit takes: few states and
+// many questions are bound by the states' bytes, one question of many by the
+// latency of a lane's chain.
 // ---------------------------------------------------------------------------
-constexpr int kJoin = 256;
+constexpr int kJoinWaves = 4;
 
 struct Part {
   float m, l;
@@ -472,50 +549,76 @@ __device__ __forceinline__ void join(Part& a, float m, float l, const f32x4_t& o
   a.m = top;
 }
 
+// The value of the lane 16 (32) away.
+__device__ __forceinline__ float far16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+}
+__device__ __forceinline__ float far32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(kJoin) void paged_join_kernel(PagedAttendParams p) {
-  __shared__ float part[kJoin * 6];
-  const int i = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttendParams p, int units) {
+  constexpr int L = D / 4, IN = 64 / L, BATCH = 4;   // lanes of a state; states a wave reads at once
+  __shared__ float part[kJoinWaves][64][6];
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (!plan_fits(p)) return;
-  scalar_words w = scalars(p.plan + p.quest + static_cast<int64_t>(i) * kQuestionWords);
-  if (w[0] == 0) return;
-  const int row0 = w[1], n0 = w[2], step0 = w[3], row1 = w[4], n1 = w[5], n = n0 + n1;
-  const int items = p.G * (D / 4);
-  int phases = 1;
-  while (items * phases * 2 <= kJoin && phases < n) phases *= 2;
-  const int64_t base = static_cast<int64_t>(g) * p.rows;
-  for (int item0 = 0; item0 < items; item0 += kJoin / phases) {
-    const int per = min(items, kJoin / phases);
-    const int item = item0 + static_cast<int>(threadIdx.x) % per, ph = threadIdx.x / per;
-    const bool on = item < items && ph < phases;
-    const int h = item / (D / 4), d = (item % (D / 4)) * 4;
+  const int most = scalars(p.plan)[9];               // states of the widest question
+  const int wpu = most <= 2 * BATCH * IN ? 1 : most <= 4 * BATCH * IN ? 2 : 4;
+  const int sub = wave & (wpu - 1), per = kJoinWaves / wpu;
+  const int d = (lane % L) * 4, phase = sub * IN + lane / L, phases = wpu * IN;
+  for (int u0 = blockIdx.x * per; u0 < units; u0 += gridDim.x * per) {
+    const int u = u0 + wave / wpu;
+    const int i = u / p.Hq, hq = u - i * p.Hq, g = hq / p.G, h = hq - g * p.G;
+    scalar_words w = scalars(p.plan + p.quest + static_cast<int64_t>(min(i, p.Nt - 1)) * kQuestionWords);
+    const bool served = u < units && w[0] != 0;
+    const int row0 = w[1] + h, step0 = w[3], row1 = w[4] + h, n0 = served ? w[2] : 0, n = served ? n0 + w[5] : 0;
+    const int64_t base = static_cast<int64_t>(g) * p.rows;
     Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     bool bad = false;
-    if (on) {
-#pragma unroll 4
-      for (int k = ph; k < n; k += phases) {
-        const int64_t row = base + h + (k < n0 ? row0 + static_cast<int64_t>(k) * step0 : row1 + static_cast<int64_t>(k - n0) * p.G);
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row);
-        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d);
-        bad = bad || ml.y < 0.f;
-        join(a, ml.x, ml.y, o, p.c);
+    for (int k0 = phase; k0 < n; k0 += phases * BATCH) {
+      float2 ml[BATCH];
+      f32x4_t o[BATCH];
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {              // all of them in flight; past the last, the last again
+        const int k = min(k0 + x * phases, n - 1);
+        const int64_t row = base + (k < n0 ? row0 + static_cast<int64_t>(k) * step0 : row1 + static_cast<int64_t>(k - n0) * p.G);
+        ml[x] = *reinterpret_cast<const float2*>(p.part_ml + 2 * row);
+        o[x] = *reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d);
       }
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x)
+        if (k0 + x * phases < n) {
+          bad = bad || ml[x].y < 0.f;
+          join(a, ml[x].x, ml[x].y, o[x], p.c);
+        }
     }
-    if (__syncthreads_or(bad)) return;               // a page outside the pool: no output
-    if (phases > 1) {
-      float* mine = part + threadIdx.x * 6;
-      mine[0] = a.m; mine[1] = a.l;
+    // a page outside the pool in any state: no output
+    float flag = bad ? 1.f : 0.f;
+    flag = fmaxf(flag, far32(flag));
+    if constexpr (IN == 4) {
+      join(a, far16(a.m), far16(a.l), f32x4_t{far16(a.o[0]), far16(a.o[1]), far16(a.o[2]), far16(a.o[3])}, p.c);
+      flag = fmaxf(flag, far16(flag));
+    }
+    join(a, far32(a.m), far32(a.l), f32x4_t{far32(a.o[0]), far32(a.o[1]), far32(a.o[2]), far32(a.o[3])}, p.c);
+    if (wpu > 1) {
+      __syncthreads();                               // the last unit's parts have been read
+      float* mine = part[wave][lane];
+      mine[0] = a.m; mine[1] = flag > 0.f ? -1.f : a.l;
 #pragma unroll
       for (int v = 0; v < 4; ++v) mine[2 + v] = a.o[v];
       __syncthreads();
-      if (on && ph == 0)
-        for (int k = 1; k < phases; ++k) {
-          const float* x = part + (threadIdx.x + k * per) * 6;
+      if (sub == 0)
+        for (int k = 1; k < wpu; ++k) {
+          const float* x = part[wave + k][lane];
+          flag = x[1] < 0.f ? 1.f : flag;
           join(a, x[0], x[1], f32x4_t{x[2], x[3], x[4], x[5]}, p.c);
         }
     }
-    if (on && ph == 0) {
-      const int64_t at = static_cast<int64_t>(i) * p.Hq + g * p.G + h;
+    if (served && sub == 0 && lane < L && flag == 0.f) {
+      const int64_t at = static_cast<int64_t>(i) * p.Hq + hq;
       const float inv = a.l == 0.f ? 0.f : 1.f / a.l;      // no keys at all: zeros, and lse -inf
       T* dst = static_cast<T*>(p.out) + at * D + d;
       if constexpr (sizeof(T) == 4) {
@@ -539,7 +642,9 @@ hipError_t launch(const PagedAttendParams& p, hipStream_t s) {
   else paged_attend_kernel<T, D, NW, NS, RB, false><<<grid, 64 * NW, 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  paged_join_kernel<T, D><<<static_cast<unsigned>(p.Nt) * p.Hkv, kJoin, 0, s>>>(p);
+  // at most a chip full of workgroups, which then go on to further units
+  const int units = p.Nt * p.Hq;
+  paged_join_kernel<T, D><<<static_cast<unsigned>(std::min(units, 2048)), 64 * kJoinWaves, 0, s>>>(p, units);
   return hipGetLastError();
 }
 

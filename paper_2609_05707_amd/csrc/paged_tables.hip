@@ -352,11 +352,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __shared__ int len_l[N], start_l[N], rank_l[N], list_l[N];
   __shared__ int4 prompt_l[N];
   __shared__ int2 where_l[N];
+  __shared__ int widest;                             // most states of a question
   const int tid = threadIdx.x, threads = blockDim.x, B = p.B, Nt = p.Nt, G = p.G;
   int32_t* plan = p.plan;
   int4* task1 = reinterpret_cast<int4*>(plan + p.task1);
   Scan scan = {sums, 0};
   scan.clear();
+  if (tid == 0) widest = 0;
   auto len = [&](int s) { return LDS ? len_l[s] : p.seq_len[s]; };
   auto start = [&](int b) { return LDS ? start_l[b] : p.q_start[b]; };
   auto rank = [&](int i) -> int& { return LDS ? rank_l[i] : plan[p.rank + i]; };
@@ -496,6 +498,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
       }
     } else if (x < B + nact) {
       *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(seq - B) * kQuestionWords + 4) = make_int4(row, np, 0, 0);
+      if constexpr (LDS) list_l[q] = np;             // (read by this thread alone until here)
     }
     tasks += ntask;
     rows += nrow;
@@ -504,6 +507,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __syncthreads();                                   // states of contexts
 
   // where the states of each question's context are
+  int most = 0;
   for (int i = tid; i < Nt; i += threads) {
     const int k = rank(i);
     int4 rec = make_int4(0, 0, 0, 0);
@@ -526,14 +530,17 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
         rec.z = pr.z;
         rec.w = (rank(start(lo + 1)) - pr.w) * G;
       }
+      most = max(most, rec.z + (LDS ? list_l[k] : plan[p.quest + static_cast<int64_t>(i) * kQuestionWords + 5]));
     }
     *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(i) * kQuestionWords) = rec;
   }
+  if (most > 0) atomicMax(&widest, most);
+  __syncthreads();
   if (tid == 0) {
     int4* head = reinterpret_cast<int4*>(plan);
     head[0] = make_int4(kPlanMagic, B, Nt, p.W);
     head[1] = make_int4(p.group_q, G, n1, n2);
-    head[2] = make_int4(p.max_len, 0, 0, 0);
+    head[2] = make_int4(p.max_len, widest, 0, 0);
   }
   if (bad && tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
