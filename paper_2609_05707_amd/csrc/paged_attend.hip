@@ -356,50 +356,53 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
 }
 
 // ---------------------------------------------------------------------------
-// Wave line: a wave streams its piece's tiles through its registers.  The next
-// tile's keys and values are in flight while it computes one, across the ends
-// of tasks too (a short segment is a tile or two): the page ids run two tiles
-// ahead, the record of the next task a task ahead, all by scalar loads.  Loads
-// of a last tile stay within the sequence's tokens, so that a segment costs the
-// bytes it has.
+// Wave line: a wave streams its piece's tiles through its registers.  The keys
+// and values of DEPTH further tiles are in flight while it computes one, across
+// the ends of tasks too (a short segment is a tile or two): the page ids run a
+// tile ahead of the loads, the record of the next task a task ahead, all by
+// scalar loads.  Every tile issues the same loads, behind the piece's last tile
+// that one's again: the compiler counts them to know what is still in flight,
+// and a load under a condition would make it wait for all.  Loads of a last
+// tile stay within the sequence's tokens, so that a segment costs the bytes it has.
 // ---------------------------------------------------------------------------
-// A tile of a piece: its task and the tile within it.
+// A tile of a piece: its task's sequence, its tokens and tiles, and the tile within
+// it.  (What else the task's record holds is read when it is needed, so that the
+// places fit the scalar registers.)
 struct Place {
-  Task task;
-  int index, tile;
+  int seq, len, tiles, index, tile;
+  __device__ __forceinline__ void load(const PagedAttendParams& p, int i) {
+    scalar_words w = scalars(p.plan + p.task2 + static_cast<int64_t>(i) * kTaskWords);
+    seq = w[0]; len = w[1]; tiles = w[6]; index = i; tile = 0;
+  }
 };
 
 template <bool SMALL>
 __device__ __forceinline__ int2 page_ids(const PagedAttendParams& p, const Place& at) {
-  scalar_words table = scalars(p.block_table + static_cast<int64_t>(at.task.seq) * p.table_pages);
-  const int shift = SMALL ? 4 : p.page_shift, a = (at.tile << 5) >> shift, last = (at.task.len - 1) >> shift;
+  scalar_words table = scalars(p.block_table + static_cast<int64_t>(at.seq) * p.table_pages);
+  const int shift = SMALL ? 4 : p.page_shift, a = (at.tile << 5) >> shift, last = (at.len - 1) >> shift;
   const int x = table[min(a, last)];
   return make_int2(x, SMALL ? table[min(a + 1, last)] : x);
 }
 
-template <typename T, int D, bool SMALL>
+template <typename T, int D, int DEPTH, bool SMALL>
 __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece, int g, int lane) {
   using M = Mfma<T>;
   const int lr = lane & 15, lg = lane >> 4;
   scalar_words pw = scalars(p.plan + p.piece2 + static_cast<int64_t>(piece) * kPieceWords);
   const int n = pw[2];
-  Place now, next, far;                              // computed, loaded, page ids read
-  Task after;                                        // the task behind far's
-  now.index = pw[0];
-  now.tile = pw[1];
-  now.task.load(p.plan, p.task2 + static_cast<int64_t>(now.index) * kTaskWords);
-  after.load(p.plan, p.task2 + static_cast<int64_t>(now.index + 1) * kTaskWords);
+  Place at[DEPTH + 2];                               // of tiles t .. t + DEPTH + 1 (behind the last: that one again)
+  Place after;                                       // the start of the task behind the furthest place's
+  at[0].load(p, pw[0]);
+  at[0].tile = pw[1];
   // (the record behind a line's last task is within the plan, and not used)
-  auto advance = [&](Place& at) {
-    if (++at.tile < at.task.tiles) return;
-    at.task = after;
-    at.tile = 0;
-    ++at.index;
-    after.load(p.plan, p.task2 + static_cast<int64_t>(at.index + 1) * kTaskWords);
-  };
-  // the place of tile t, or, behind the piece's last, that one again
-  auto follow = [&](Place& at, int t) {
-    if (t < n) advance(at);
+  after.load(p, at[0].index + 1);
+  auto follow = [&](const Place& from, int t) {      // the place of tile t, behind `from`
+    Place to = from;
+    if (t >= n) return to;
+    if (++to.tile < to.tiles) return to;
+    to = after;
+    after.load(p, to.index + 1);
+    return to;
   };
   auto checked = [&](int2 id, bool& no) {
     no = static_cast<uint32_t>(id.x) >= static_cast<uint32_t>(p.num_pages) ||
@@ -411,93 +414,108 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   // are the second page's
   const int ktok = tile_token(0, lr);
   auto base_of = [&](const void* pages, int2 id, int tile, int& tok) {
-    int64_t at = page_at<SMALL, D>(p, id.x, g, tile);
+    int64_t base = page_at<SMALL, D>(p, id.x, g, tile);
     if (SMALL && tok >= 16) {
-      at = page_at<SMALL, D>(p, id.y, g, tile);
+      base = page_at<SMALL, D>(p, id.y, g, tile);
       tok -= 16;
     }
-    return static_cast<const T*>(pages) + at;
+    return static_cast<const T*>(pages) + base;
   };
-  typename M::Frag qf[D / 32], qn[D / 32], kf[2][D / 32], vf[D / 16];
-  auto load_keys = [&](const Place& at, int2 id) {
-    const int lim = at.task.len - 1 - 32 * at.tile;
+  struct Set {                                       // a tile in flight, with its rows' queries
+    typename M::Frag q[D / 32], k[2][D / 32], v[D / 16];
+    bool bad;                                        // its page lies outside the pool
+  } set[DEPTH];
+  auto load_keys = [&](Set& f, const Place& x, int2 id) {
+    const int lim = x.len - 1 - 32 * x.tile;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       int tok = min(ktok + 4 * kb, lim);
-      const T* src = base_of(p.k_pages, id, at.tile, tok) + tok * D + 8 * lg;
+      const T* src = base_of(p.k_pages, id, x.tile, tok) + tok * D + 8 * lg;
 #pragma unroll
-      for (int ds = 0; ds < D / 32; ++ds) kf[kb][ds] = M::load(src + 32 * ds);
+      for (int ds = 0; ds < D / 32; ++ds) f.k[kb][ds] = M::load(src + 32 * ds);
     }
   };
-  auto load_values = [&](const Place& at, int2 id) {
-    int tok = 8 * min(lg, (at.task.len - 1 - 32 * at.tile) >> 3);
-    const T* src = base_of(p.v_pages, id, at.tile, tok) + tok * D + 8 * lr;
+  auto load_values = [&](Set& f, const Place& x, int2 id) {
+    int tok = 8 * min(lg, (x.len - 1 - 32 * x.tile) >> 3);
+    const T* src = base_of(p.v_pages, id, x.tile, tok) + tok * D + 8 * lr;
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) vf[db] = M::load(src + 128 * db);
+    for (int db = 0; db < D / 16; ++db) f.v[db] = M::load(src + 128 * db);
   };
-  auto load_rows = [&](const Task& task, typename M::Frag (&f)[D / 32]) {
-    const int r = min(lr, task.rows - 1);
-    int i = task.seq - p.B, h = r;                   // a segment's rows are its question's heads
-    if (task.seq < p.B) {
-      i = p.plan[p.qlist + task.q + r / p.G];
+  auto load_rows = [&](Set& f, const Place& x) {
+    int i = x.seq - p.B, h = min(lr, p.G - 1);       // a segment's rows are its question's heads
+    if (x.seq < p.B) {
+      scalar_words w = scalars(p.plan + p.task2 + static_cast<int64_t>(x.index) * kTaskWords);
+      const int r = min(lr, w[2] - 1);
+      i = p.plan[p.qlist + w[3] + r / p.G];
       h = r % p.G;
+      asm volatile("" : "+v"(i));                    // waited for here, not where a segment passes too
     }
     const T* src = static_cast<const T*>(p.q_rot) + (static_cast<int64_t>(i) * p.Hq + g * p.G + h) * D + 8 * lg;
 #pragma unroll
-    for (int ds = 0; ds < D / 32; ++ds) f[ds] = M::load(src + 32 * ds);
+    for (int ds = 0; ds < D / 32; ++ds) f.q[ds] = M::load(src + 32 * ds);
   };
-  int2 id = page_ids<SMALL>(p, now);
-  far = now;
-  follow(far, 1);
-  int2 ahead = page_ids<SMALL>(p, far);
-  load_rows(now.task, qf);
-  bool bad, bad_next;                                // of the task computed; of the tile loaded
-  id = checked(id, bad);
-  bool any = bad;
-  load_keys(now, id);
-  load_values(now, id);
-  next = far;
+  int2 id = page_ids<SMALL>(p, at[0]);
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) {
+    at[d + 1] = follow(at[d], d + 1);
+    const int2 ahead = page_ids<SMALL>(p, at[d + 1]);
+    id = checked(id, set[d].bad);
+    // in the loop's order: the waits there are for the worse of both
+    load_rows(set[d], at[d]);
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(set[d], at[d], id);
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(set[d], at[d], id);
+    __builtin_amdgcn_sched_barrier(0);
+    id = ahead;
+  }
+  bool bad = false, any = false;
   State<D> st;
   clear(st);
-  for (int t = 0; t < n; ++t) {
-    const bool ends = t + 1 >= n || next.index != now.index;   // the last tile of its task here
-    const bool more = t + 1 < n;
-    id = checked(ahead, bad_next);
-    any = any || bad_next;
-    follow(far, t + 2);
-    ahead = page_ids<SMALL>(p, far);
-    if (more && ends) load_rows(next.task, qn);
-    f32x4_t sc[2];
+  for (int t0 = 0; t0 < n; t0 += DEPTH) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      sc[kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DEPTH; ++d) {
+      const int t = t0 + d;
+      if (t >= n) break;
+      Set& f = set[d];
+      const bool ends = t + 1 >= n || at[1].index != at[0].index;   // the last tile of its task here
+      bad = bad || f.bad;
+      id = checked(id, f.bad);
+      at[DEPTH + 1] = follow(at[DEPTH], t + DEPTH + 1);
+      const int2 ahead = page_ids<SMALL>(p, at[DEPTH + 1]);
+      f32x4_t sc[2];
 #pragma unroll
-      for (int ds = 0; ds < D / 32; ++ds) sc[kb] = M::mma(kf[kb][ds], qf[ds], sc[kb]);
+      for (int kb = 0; kb < 2; ++kb) {
+        sc[kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ds = 0; ds < D / 32; ++ds) sc[kb] = M::mma(f.k[kb][ds], f.q[ds], sc[kb]);
+      }
+      if (at[DEPTH].index != at[0].index) load_rows(f, at[DEPTH]);
+      load_keys(f, at[DEPTH], id);
+      const int m = at[0].len - 32 * at[0].tile;
+      if (m < 32) mask_scores(sc, m, lg);
+      const typename M::Frag pf = fold<T, D>(sc, st, p.c);
+      if (m < 32) {                                  // what lies past the end may be anything
+        const int keep = min(max(m - 8 * lg, 0), 8);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) f.v[db] = M::keep_first(f.v[db], keep);
+      }
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) st.o[db] = M::mma(f.v[db], pf, st.o[db]);
+      load_values(f, at[DEPTH], id);
+      if (ends) {
+        Task task;
+        task.load(p.plan, p.task2 + static_cast<int64_t>(at[0].index) * kTaskWords);
+        const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
+        publish<D>(p, st, row + lr, lr < task.rows, bad, lg);
+        any = any || bad;
+        bad = false;
+        clear(st);
+      }
+      id = ahead;
+#pragma unroll
+      for (int k = 0; k <= DEPTH; ++k) at[k] = at[k + 1];
     }
-    if (more) load_keys(next, id);
-    const int m = now.task.len - 32 * now.tile;
-    if (m < 32) mask_scores(sc, m, lg);
-    const typename M::Frag pf = fold<T, D>(sc, st, p.c);
-    if (m < 32) {                                    // what lies past the end may be anything
-      const int keep = min(max(m - 8 * lg, 0), 8);
-#pragma unroll
-      for (int db = 0; db < D / 16; ++db) vf[db] = M::keep_first(vf[db], keep);
-    }
-#pragma unroll
-    for (int db = 0; db < D / 16; ++db) st.o[db] = M::mma(vf[db], pf, st.o[db]);
-    if (more) load_values(next, id);
-    if (ends) {
-      const int64_t row = static_cast<int64_t>(g) * p.rows + now.task.row +
-                          static_cast<int64_t>(piece - now.task.first) * now.task.rows;
-      publish<D>(p, st, row + lr, lr < now.task.rows, bad, lg);
-      bad = false;
-      clear(st);
-#pragma unroll
-      for (int ds = 0; ds < D / 32; ++ds) qf[ds] = qn[ds];
-    }
-    bad = bad || bad_next;
-    now = next;
-    next = far;
   }
   if (any && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
@@ -509,6 +527,9 @@ __device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
          h[8] == p.table_pages << p.page_shift;
 }
 
+#ifndef WDEPTH
+#define WDEPTH 2
+#endif
 template <typename T, int D, int NW, int NS, int RB, bool SMALL>
 __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendParams p) {
   __shared__ __attribute__((aligned(1024))) unsigned char ring[NS * Ring<T, D, NS>::STAGE];
@@ -524,7 +545,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendPar
     return;
   }
   const int piece = wave * (p.W - n1) + (b - n1);
-  if (piece < n2) wave_piece<T, D, SMALL>(p, piece, g, lane);
+  if (piece < n2) wave_piece<T, D, (sizeof(T) * D > 256 ? 1 : WDEPTH), SMALL>(p, piece, g, lane);
 }
 
 // ---------------------------------------------------------------------------
