@@ -101,31 +101,50 @@ __device__ __forceinline__ void load_query(const PagedAttendParams& p, typename 
   for (int ds = 0; ds < D / 32; ++ds) qf[ds] = Mfma<T>::load(src + 32 * ds);
 }
 
-// Pages of the tiles of one sequence.  A tile lies in one page, or at 16 tokens
-// a page in two, of which the second may not exist: it then stands for the first.
-template <bool SMALL>
+// Where the tiles of one sequence lie, for kv head g.  A tile lies in one page, or
+// at 16 tokens a page in two, of which the second may not exist: it then stands
+// for the first.  (All of it in scalar registers: a step of the block line has
+// few instructions besides its products.)
+template <typename T, int D, bool SMALL>
 struct Pages {
   scalar_words table;
+  const char* k; const char* v;                      // head g's part of page 0
+  uint32_t stride;                                   // bytes of a page, all heads
   int shift, most, last;                             // pages of the pool; the sequence's last page
   bool bad;
-  __device__ __forceinline__ void init(const PagedAttendParams& p, int seq, int len) {
+  __device__ __forceinline__ void init(const PagedAttendParams& p, int seq, int len, int g) {
+    constexpr int ROW = D * static_cast<int>(sizeof(T));
     table = scalars(p.block_table + static_cast<int64_t>(seq) * p.table_pages);
     shift = SMALL ? 4 : p.page_shift;
     most = p.num_pages;
     last = (len - 1) >> shift;
+    stride = (static_cast<uint32_t>(p.Hkv) << shift) * ROW;
+    const uint64_t head = (static_cast<uint64_t>(g) << shift) * ROW;
+    k = static_cast<const char*>(p.k_pages) + head;
+    v = static_cast<const char*>(p.v_pages) + head;
     bad = false;
   }
-  // Page ids of tile t (the second is the first's unless SMALL).
+  // Page ids of tile t of the sequence (the second is the first's unless SMALL).
   __device__ __forceinline__ int2 of(int t) const {
-    const int a = (t << 5) >> shift;
-    const int x = table[min(a, last)];
-    return make_int2(x, SMALL ? table[min(a + 1, last)] : x);
+    if constexpr (!SMALL) {
+      const int x = table[t >> (shift - 5)];
+      return make_int2(x, x);
+    } else {
+      return make_int2(table[2 * t], table[min(2 * t + 1, last)]);
+    }
   }
   __device__ __forceinline__ int2 checked(int2 id) {
     const bool no = static_cast<uint32_t>(id.x) >= static_cast<uint32_t>(most) ||
                     (SMALL && static_cast<uint32_t>(id.y) >= static_cast<uint32_t>(most));
     bad = bad || no;
     return no ? make_int2(0, 0) : id;
+  }
+  // Bytes from k (v) to page `id`, and to tile t's tokens in it.
+  __device__ __forceinline__ uint64_t at(int id, int t) const {
+    const uint64_t page = static_cast<uint64_t>(static_cast<uint32_t>(id)) * stride;
+    if constexpr (SMALL) return page;
+    const uint32_t t0 = (static_cast<uint32_t>(t) << 5) & ((1u << shift) - 1u);
+    return page + t0 * static_cast<uint32_t>(D * sizeof(T));
   }
 };
 
@@ -144,31 +163,27 @@ __device__ __forceinline__ int64_t page_at(const PagedAttendParams& p, int id, i
 // holds rows 16 (NW j + w) .., so that few rows spread over all four SIMDs.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NW, int NS, bool SMALL>
-__device__ __forceinline__ void fetch(uint32_t stage, const PagedAttendParams& p, int2 id, int g, int tile, int wave, int lane,
+__device__ __forceinline__ void fetch(uint32_t stage, const Pages<T, D, SMALL>& pages, int2 id, int tile, int wave,
                                       const TileOffsets<T, D, NW, NS>& to) {
   using R = Ring<T, D, NS>;
   constexpr int DPT = R::BLOCKS / NW;
-  const int64_t a = page_at<SMALL, D>(p, id.x, g, tile);
-  const T* ka = static_cast<const T*>(p.k_pages) + a;
-  const T* va = static_cast<const T*>(p.v_pages) + a;
+  const uint64_t a = pages.at(id.x, tile);
   if constexpr (!SMALL) {
 #pragma unroll
     for (int d = 0; d < DPT; ++d) {
       const int q = wave + NW * d;                   // wave-uniform
-      dma16s(q < R::KBLOCKS ? ka : va, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
+      dma16s((q < R::KBLOCKS ? pages.k : pages.v) + a, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
     }
   } else {
     // the offsets are those of a whole tile: tokens 16 .. 31 sit at the second page's start
     constexpr int HALF = 16 * D * R::E;
-    const int64_t b = page_at<SMALL, D>(p, id.y, g, tile);
-    const T* kb = static_cast<const T*>(p.k_pages) + b;
-    const T* vb = static_cast<const T*>(p.v_pages) + b;
+    const uint64_t b = pages.at(id.y, tile);
 #pragma unroll
     for (int d = 0; d < DPT; ++d) {
       const int q = wave + NW * d;
       const bool second = to.off[d] >= HALF;
-      const char* base = reinterpret_cast<const char*>(q < R::KBLOCKS ? (second ? kb : ka) : (second ? vb : va));
-      dma16(base + (to.off[d] - (second ? HALF : 0)), stage + static_cast<uint32_t>(q) * 1024u);
+      dma16((q < R::KBLOCKS ? pages.k : pages.v) + (second ? b - HALF : a) + to.off[d],
+            stage + static_cast<uint32_t>(q) * 1024u);
     }
   }
 }
@@ -268,12 +283,12 @@ __device__ __forceinline__ void step(const unsigned char* stk, const unsigned ch
 // fetches).  Waves of a workgroup differ in RL and meet at the same barriers.
 template <typename T, int D, int NW, int NS, int RL, bool SMALL>
 __device__ __forceinline__ void stream(const PagedAttendParams& p, unsigned char* ring, const Task& task, int g, int tile,
-                                       int n, int64_t row, Pages<SMALL>& pages, int wave, int lane,
+                                       int n, int64_t row, Pages<T, D, SMALL>& pages, int wave, int lane,
                                        const TileOffsets<T, D, NW, NS>& to) {
   using R = Ring<T, D, NS>;
   using M = Mfma<T>;
-  constexpr int DPT = R::BLOCKS / NW, RB = RL ? RL : 1;
-  const int lr = lane & 15, lg = lane >> 4;
+  constexpr int DPT = R::BLOCKS / NW, RB = RL ? RL : 1, WRAP = NS * R::STAGE;
+  const int lr = lane & 15, lg = lane >> 4, last = n - 1;
   const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
   typename M::Frag qf[RB][D / 32];
   State<D> st[RB];
@@ -284,40 +299,58 @@ __device__ __forceinline__ void stream(const PagedAttendParams& p, unsigned char
       clear(st[rb]);
     }
   }
+  const int end = tile + last;
+  int put = tile;                                    // the tile fetched next, and its pages
   int2 id = pages.of(tile);
-  auto next_fetch = [&](int t) {                     // tile t of the n
-    const int2 next = pages.of(min(tile + t + 1, task.tiles - 1));
-    fetch<T, D, NW, NS, SMALL>(lds + (t % NS) * R::STAGE, p, pages.checked(id), g, tile + t, wave, lane, to);
+  auto fetch_next = [&](int stage) {
+    const int2 next = pages.of(min(put + 1, end));
+    fetch<T, D, NW, NS, SMALL>(lds + stage, pages, pages.checked(id), put, wave, to);
     id = next;
+    ++put;
   };
-  for (int t = 0; t < NS - 1 && t < n; ++t) next_fetch(t);
-  const int last = n - 1;
+  for (int t = 0; t < NS - 1 && t < n; ++t) fetch_next(t * R::STAGE);
   // tile t is folded in step t, whose barrier also says that every wave is past
   // step t - 1; the stage of tile t - 1 then takes tile t + NS - 1.  Steps in
-  // pairs, so that the two sets of scores swap places without copies.
+  // pairs, so that the two sets of scores swap places without copies; as long as
+  // there are tiles to fetch the waits are constants.
   f32x4_t sa[RB][2], sb[RB][2];
   wait_tiles<DPT, NS - 2>(min(last, NS - 2));
   __syncthreads();
   if constexpr (RL > 0) scores<T, D, NS, RB>(ring, qf, sa, lr, lg);
-  auto half = [&](int t, f32x4_t (&now)[RB][2], f32x4_t (&then)[RB][2]) {
+  int free = (NS - 1) * R::STAGE, here = 0, then = R::STAGE;   // stages of tiles t - 1, t, t + 1
+  auto rest = [&](f32x4_t (&now)[RB][2], f32x4_t (&next)[RB][2]) {
+    if constexpr (RL > 0) step<T, D, NS, RB>(ring + then, ring + here, qf, now, next, st, lr, lg, p.c);
+    free = here;
+    here = then;
+    then = then + R::STAGE == WRAP ? 0 : then + R::STAGE;
+  };
+  auto full = [&](f32x4_t (&now)[RB][2], f32x4_t (&next)[RB][2]) {
+    wait_vmcnt<((NS - 3) * DPT < 63 ? (NS - 3) * DPT : 63)>();
+    __syncthreads();
+    fetch_next(free);
+    rest(now, next);
+  };
+  auto drain = [&](int t, f32x4_t (&now)[RB][2], f32x4_t (&next)[RB][2]) {
     wait_tiles<DPT, NS - 3>(min(last - t - 1, NS - 3));
     __syncthreads();
-    if (t + NS - 1 <= last) next_fetch(t + NS - 1);
-    if constexpr (RL > 0)
-      step<T, D, NS, RB>(ring + ((t + 1) % NS) * R::STAGE, ring + (t % NS) * R::STAGE, qf, now, then, st, lr, lg, p.c);
+    if (put <= end) fetch_next(free);
+    rest(now, next);
   };
   int t = 0;
-  for (; t + 2 <= last; t += 2) {
-    half(t, sa, sb);
-    half(t + 1, sb, sa);
+  for (; put + 1 <= end; t += 2) {
+    full(sa, sb);
+    full(sb, sa);
   }
-  const int tail = min(32, task.len - 32 * (tile + last));
-  const unsigned char* end = ring + (last % NS) * R::STAGE;
+  for (; t + 2 <= last; t += 2) {
+    drain(t, sa, sb);
+    drain(t + 1, sb, sa);
+  }
+  const int tail = min(32, task.len - 32 * end);
   if (t < last) {
-    half(t, sa, sb);
-    if constexpr (RL > 0) values<T, D, NS, RB>(end, sb, st, tail, lr, lg, p.c);
+    drain(t, sa, sb);
+    if constexpr (RL > 0) values<T, D, NS, RB>(ring + here, sb, st, tail, lr, lg, p.c);
   } else {
-    if constexpr (RL > 0) values<T, D, NS, RB>(end, sa, st, tail, lr, lg, p.c);
+    if constexpr (RL > 0) values<T, D, NS, RB>(ring + here, sa, st, tail, lr, lg, p.c);
   }
   if constexpr (RL > 0) {
 #pragma unroll
@@ -338,8 +371,8 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
     Task task;
     task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
     const int n = min(left, task.tiles - tile);
-    Pages<SMALL> pages;
-    pages.init(p, task.seq, task.len);
+    Pages<T, D, SMALL> pages;
+    pages.init(p, task.seq, task.len, g);
     const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
     if (RB == 2 && 16 * (NW + wave) < task.rows)
       stream<T, D, NW, NS, RB, SMALL>(p, ring, task, g, tile, n, row, pages, wave, lane, to);
