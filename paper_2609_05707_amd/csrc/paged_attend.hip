@@ -29,10 +29,10 @@ __device__ __forceinline__ scalar_words scalars(const int32_t* p) { return (scal
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 struct Task {
-  int seq, len, rows, q, row, first, tiles;
+  int seq, len, rows, q, row, first, tiles, lead;
   __device__ __forceinline__ void load(const int32_t* plan, int64_t at) {
     scalar_words w = scalars(plan + at);
-    seq = w[0]; len = w[1]; rows = w[2]; q = w[3]; row = w[4]; first = w[5]; tiles = w[6];
+    seq = w[0]; len = w[1]; rows = w[2]; q = w[3]; row = w[4]; first = w[5]; tiles = w[6]; lead = w[7];
   }
 };
 
@@ -366,11 +366,11 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
   TileOffsets<T, D, NW, NS> to;
   to.init(wave, lane);
   scalar_words pw = scalars(p.plan + p.piece1 + static_cast<int64_t>(piece) * kPieceWords);
-  int index = pw[0], tile = pw[1], left = pw[2];
-  while (left > 0) {
-    Task task;
-    task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
-    const int n = min(left, task.tiles - tile);
+  const int tasks = scalars(p.plan)[10];
+  int index = pw[0], tile = pw[1], n = pw[2];
+  Task task;
+  task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
+  while (true) {
     Pages<T, D, SMALL> pages;
     pages.init(p, task.seq, task.len, g);
     const int64_t row = static_cast<int64_t>(g) * p.rows + task.row + static_cast<int64_t>(piece - task.first) * task.rows;
@@ -381,9 +381,12 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
     else
       stream<T, D, NW, NS, 0, SMALL>(p, ring, task, g, tile, n, row, pages, wave, lane, to);
     if (pages.bad && wave == 0 && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
-    left -= n;
+    // the next task, if the piece goes on into it
+    if (++index >= tasks) break;
+    task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
+    if (task.first != piece) break;
     tile = 0;
-    ++index;
+    n = task.lead;
     __syncthreads();                                 // every wave is past the last tile
   }
 }

@@ -20,8 +20,9 @@ namespace ippd {
 
 constexpr int kPlanMagic = 0x49504450;    // first word of a plan
 constexpr int kPlanHeader = 64;           // words of its header
-constexpr int kPieceWords = 4;            // task, first tile within it, tiles of the piece, 0
-constexpr int kTaskWords = 8;             // sequence, tokens, rows, first active question, first state row, first piece, tiles, states (pieces)
+constexpr int kPieceWords = 4;            // first task, first tile within it, tiles (block line: of that task; wave line: in all), 0
+constexpr int kTaskWords = 8;             // sequence, tokens, rows, first active question; first state row, first piece, tiles,
+                                          // tiles in the first piece (block line)
 constexpr int kQuestionWords = 8;         // served, context state row, states, rows a state; segment state row, states; 0, 0
 constexpr int kPromptWords = 4;           // kind (0 none, 1 block line, 2 wave line); first task and questions a
                                           // group, or first state row and states; rank of its first question
@@ -36,7 +37,8 @@ struct PagedShape {
   int group_q;                            // questions of a block-line row group (0: no block line)
   int64_t rows;                           // partial states per kv head
   // word offsets of the plan's arrays
-  int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank, words;
+  int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank, where, words;
+  int block_cost;                         // a block-line tile's cost to a workgroup, in the wave line's
   size_t off_ml, workspace_bytes;
 };
 
@@ -61,7 +63,8 @@ struct PagedPlanParams {
   const int32_t* q_start; const int32_t* seq_len; const uint8_t* active; int32_t* err_flag;
   int B, Nt, G, W, waves, group_q, max_questions;
   int max_len;                            // table_pages * page_tokens
-  int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank;
+  int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank, where;
+  int block_cost;
 };
 
 struct PagedAttendParams {

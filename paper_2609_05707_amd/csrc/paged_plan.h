@@ -58,6 +58,7 @@ inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   // fp32 at head_dim 128, whose ring leaves no room for a second workgroup.
   s.waves = (bf16 ? most > 128 : bt->head_dim == 128) ? 8 : 4;
   s.rb = bf16 && most > 64 ? 2 : 1;
+  s.block_cost = bf16 ? 1 : s.waves;
   s.W = std::max(2, kPagedComputeUnits * (s.waves == 8 ? 1 : 2) / bt->num_kv_heads);
   s.group_q = most > 16 ? 16 * s.waves * s.rb / s.G : 0;
   const int64_t nt = bt->num_questions, b = bt->num_prompts, w1 = s.W, w2 = w1 * s.waves;
@@ -72,6 +73,8 @@ inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   s.prompt = at; at += b * kPromptWords;
   s.qlist = at; at += nt;
   s.rank = at; at += nt + 1;
+  at += at & 1;
+  s.where = at; at += 2 * nt;
   s.words = at;
   const size_t states = static_cast<size_t>(s.rows) * bt->num_kv_heads;
   s.off_ml = (states * bt->head_dim * 4 + 255) & ~static_cast<size_t>(255);

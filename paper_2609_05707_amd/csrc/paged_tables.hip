@@ -307,11 +307,16 @@ __global__ __launch_bounds__(256) void rows_kernel(ReserveParams p) {
 // keep it in the plan.
 // ---------------------------------------------------------------------------
 constexpr int kPlanLds = 1024;
-#ifndef KBT
-#define KBT 1
-#define KWT 1
-#endif
-constexpr int kBlockTile = KBT, kWaveTile = KWT;
+// Tiles that the start of a task costs a piece of the block line (its rows' queries
+// and the ring's first tiles, some 8 us): they count as length, so that a piece
+// in which a task begins has fewer.  8 prompts of 8192 x 32, three layers: 258 us
+// without, 248 with 4, 250 with 8.
+constexpr int kSetup = 4;
+// The shortest pieces of the block line, in tiles; longer than kSetup, so that
+// every piece has a tile.  One prompt of 4096 tokens x 16 questions, eight layers:
+// 150 us at 4 or 5, 145 at 6 and 8.
+constexpr int kShortest = 6;
+static_assert(kShortest > kSetup, "a piece may not lie between two tasks' tiles");
 
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   const uint64_t x = a, y = b;
@@ -335,17 +340,25 @@ struct Line {
   }
 };
 
-// A task of `tiles` > 0 tiles from `at` on the line, in pieces first .. first + states - 1:
-// its record, and the records of the pieces that begin inside it.
+// A task whose `tiles` > 0 tiles follow `setup` places from `at` on the line, in
+// pieces first .. first + states - 1: its record, and the records of the pieces
+// whose first tile is one of its.  A piece ends with its own places: its record
+// counts its tiles on the block line within that task (the next task's record
+// says how many of its tiles are still in the piece), on the wave line in all.
+template <bool BLOCK>
 __device__ __forceinline__ void write_task(int32_t* plan, int64_t tasks, int64_t pieces, const Line& line, int index,
                                            int64_t at, int tiles, int seq, int len, int rows, int q, int row, int first,
                                            int states) {
+  const int64_t tile0 = at + (BLOCK ? kSetup : 0);
+  auto until = [&](int p) { return static_cast<int>(min(line.start(p + 1) - tile0, static_cast<int64_t>(tiles))); };
   int4* t = reinterpret_cast<int4*>(plan + tasks + static_cast<int64_t>(index) * kTaskWords);
   t[0] = make_int4(seq, len, rows, q);
-  t[1] = make_int4(row, first, tiles, states);
-  for (int p = line.start(first) == at ? first : first + 1; p < first + states; ++p)
+  t[1] = make_int4(row, first, tiles, BLOCK ? until(first) : 0);
+  for (int p = line.start(first) >= at ? first : first + 1; p < first + states; ++p) {
+    const int tile = static_cast<int>(max(line.start(p) - tile0, static_cast<int64_t>(0)));
     *reinterpret_cast<int4*>(plan + pieces + static_cast<int64_t>(p) * kPieceWords) =
-        make_int4(index, static_cast<int>(line.start(p) - at), static_cast<int>(line.start(p + 1) - line.start(p)), 0);
+        make_int4(index, tile, BLOCK ? until(p) - tile : static_cast<int>(line.start(p + 1) - line.start(p)), 0);
+  }
 }
 
 __device__ __forceinline__ int tiles_of(int len) { return static_cast<int>((static_cast<uint32_t>(len) + 31u) >> 5); }
@@ -360,7 +373,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __shared__ int widest;                             // most states of a question
   const int tid = threadIdx.x, threads = blockDim.x, B = p.B, Nt = p.Nt, G = p.G;
   int32_t* plan = p.plan;
-  int4* task1 = reinterpret_cast<int4*>(plan + p.task1);
+  int2* where = reinterpret_cast<int2*>(plan + p.where);   // first state row and states of the block line's tasks
   Scan scan = {sums, 0};
   scan.clear();
   if (tid == 0) widest = 0;
@@ -405,22 +418,22 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   if (!bad) {
     for (int b = tid; b < B; b += threads) {
       const int n = rank(start(b + 1)) - rank(start(b)), tiles = tiles_of(len(b));
-      if (p.group_q > 0 && n * G > 16) t1 += static_cast<int64_t>((n + p.group_q - 1) / p.group_q) * tiles;
+      if (p.group_q > 0 && n * G > 16) t1 += static_cast<int64_t>((n + p.group_q - 1) / p.group_q) * (tiles > 0 ? tiles + kSetup : 0);
       else if (n > 0) t2 += tiles;
     }
     for (int k = tid; k < nact; k += threads) t2 += tiles_of(len(B + list(k)));
   }
   scan(t1, t2, T1, T2);
-  // workgroups to the lines by their shares of the work, runs of four tiles
-  // at least on the block line and of two on the wave line.  A tile takes a
-  // workgroup about kBlockTile / kWaveTile as long as it takes a wave: 1.4 us
-  // (128 rows, four waves) against 2.4.
+  // workgroups to the lines by their shares of the work, runs of two tiles at
+  // least on the wave line.  Bound by the stream (bf16) a tile costs a workgroup
+  // the same on either line (twice as much on the block line: 8 prompts of 8192
+  // x 32 248 -> 269 us, three layers); bound by the products (fp32) a workgroup
+  // does as many tiles on the wave line as it has waves.
   int n1 = 0, n2 = 0;
   if (T1 > 0) {
-    const int64_t most = p.W - (T2 > 0 ? 1 : 0);
-    const int64_t c1 = T1 * kBlockTile, c2 = T2 * kWaveTile;
-    const int64_t share = quotient(c1 * p.W + (c1 + c2) / 2, c1 + c2);
-    n1 = static_cast<int>(min(max(min(share, (T1 + 3) / 4), static_cast<int64_t>(1)), most));
+    const int64_t most = p.W - (T2 > 0 ? 1 : 0), c1 = T1 * p.block_cost;
+    const int64_t share = quotient(c1 * p.W + (c1 + T2) / 2, c1 + T2);
+    n1 = static_cast<int>(min(max(min(share, T1 / kShortest), static_cast<int64_t>(1)), most));
   }
   if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(p.waves) * (p.W - n1), (T2 + 1) / 2));
   const Line line1(T1, n1), line2(T2, n2);
@@ -444,23 +457,24 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
       }
     }
     const int tiles = tiles_of(tokens);
-    int64_t task0 = groups, at0 = static_cast<int64_t>(groups) * tiles, ntask, ntile;
+    int64_t task0 = groups, at0 = static_cast<int64_t>(groups) * (tiles + kSetup), ntask, ntile;
     scan(task0, at0, ntask, ntile);
     task0 += tasks;
     at0 += at;
     int need = 0;
     for (int j = 0; j < groups; ++j) {
-      const int64_t x = at0 + static_cast<int64_t>(j) * tiles;
-      need += (line1.piece_of(x + tiles - 1) - line1.piece_of(x) + 1) * (min(per, n - j * per) * G);
+      const int64_t x = at0 + static_cast<int64_t>(j) * (tiles + kSetup);
+      need += (line1.piece_of(x + kSetup + tiles - 1) - line1.piece_of(x + kSetup) + 1) * (min(per, n - j * per) * G);
     }
     int nrow;
     int row = rows + scan(need, nrow);
     for (int j = 0; j < groups; ++j) {
-      const int64_t x = at0 + static_cast<int64_t>(j) * tiles;
-      const int gr = min(per, n - j * per) * G, first = line1.piece_of(x), states = line1.piece_of(x + tiles - 1) - first + 1;
+      const int64_t x = at0 + static_cast<int64_t>(j) * (tiles + kSetup);
+      const int gr = min(per, n - j * per) * G, first = line1.piece_of(x + kSetup);
+      const int states = line1.piece_of(x + kSetup + tiles - 1) - first + 1;
       const int t = static_cast<int>(task0) + j;
-      write_task(plan, p.task1, p.piece1, line1, t, x, tiles, b, tokens, gr, r0 + j * per, row, first, states);
-      if constexpr (LDS) where_l[t] = make_int2(row, states);
+      write_task<true>(plan, p.task1, p.piece1, line1, t, x, tiles, b, tokens, gr, r0 + j * per, row, first, states);
+      (LDS ? where_l[t] : where[t]) = make_int2(row, states);
       row += states * gr;
     }
     if (b < B) prompt(b) = make_int4(kind, static_cast<int>(task0), per, r0);
@@ -468,6 +482,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     rows += nrow;
     at += ntile;
   }
+  const int block_tasks = static_cast<int>(tasks);
   __syncthreads();                                   // prompts
 
   // wave line: the other contexts, then the segments of the active questions
@@ -498,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     int nrow;
     const int row = rows + scan(np * n, nrow);
     if (tiles > 0)
-      write_task(plan, p.task2, p.piece2, line2, static_cast<int>(task), at0, tiles, seq, tokens, n, q, row, first, np);
+      write_task<false>(plan, p.task2, p.piece2, line2, static_cast<int>(task), at0, tiles, seq, tokens, n, q, row, first, np);
     if (x < B) {
       if (seq >= 0) {
         prompt(x).y = row;
@@ -529,9 +544,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
       rec.x = 1;
       if (pr.x == 1) {                               // (first task, questions a group)
         const int local = k - pr.w, j = local / pr.z;
-        const int4 tb = LDS ? make_int4(where_l[pr.y + j].x, 0, 0, where_l[pr.y + j].y) : task1[2 * (pr.y + j) + 1];
-        rec.y = tb.x + (local - j * pr.z) * G;
-        rec.z = tb.w;
+        const int2 at1 = LDS ? where_l[pr.y + j] : where[pr.y + j];
+        rec.y = at1.x + (local - j * pr.z) * G;
+        rec.z = at1.y;
         rec.w = min(pr.z, rank(start(lo + 1)) - pr.w - j * pr.z) * G;
       } else if (pr.x == 2) {                        // (first state's row, states)
         rec.y = pr.y + (k - pr.w) * G;
@@ -548,7 +563,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     int4* head = reinterpret_cast<int4*>(plan);
     head[0] = make_int4(kPlanMagic, B, Nt, p.W);
     head[1] = make_int4(p.group_q, G, n1, n2);
-    head[2] = make_int4(p.max_len, widest, 0, 0);
+    head[2] = make_int4(p.max_len, widest, block_tasks, 0);
   }
   if (bad && tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
