@@ -162,6 +162,18 @@ __device__ __forceinline__ int64_t page_at(const PagedAttendParams& p, int id, i
 // Every fragment read from LDS serves the wave's row blocks.  Block j of wave w
 // holds rows 16 (NW j + w) .., so that few rows spread over all four SIMDs.
 // ---------------------------------------------------------------------------
+// dma16s and dma16 with the non-temporal hint: a context's tiles are read once, and
+// as ordinary lines they push each other and the partial states out of the caches
+// (8 prompts of 8192 x 32, three layers: 250 us without it, 227 with).
+__device__ __forceinline__ void stream16s(const void* sbase, uint32_t voff, uint32_t lds_block) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :: "v"(voff), "s"(sbase), "{m0}"(__builtin_amdgcn_readfirstlane(lds_block)) : "memory");
+}
+__device__ __forceinline__ void stream16(const void* gptr, uint32_t lds_block) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
+               :: "v"(gptr), "{m0}"(__builtin_amdgcn_readfirstlane(lds_block)) : "memory");
+}
+
 template <typename T, int D, int NW, int NS, bool SMALL>
 __device__ __forceinline__ void fetch(uint32_t stage, const Pages<T, D, SMALL>& pages, int2 id, int tile, int wave,
                                       const TileOffsets<T, D, NW, NS>& to) {
@@ -172,7 +184,7 @@ __device__ __forceinline__ void fetch(uint32_t stage, const Pages<T, D, SMALL>& 
 #pragma unroll
     for (int d = 0; d < DPT; ++d) {
       const int q = wave + NW * d;                   // wave-uniform
-      dma16s((q < R::KBLOCKS ? pages.k : pages.v) + a, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
+      stream16s((q < R::KBLOCKS ? pages.k : pages.v) + a, to.off[d], stage + static_cast<uint32_t>(q) * 1024u);
     }
   } else {
     // the offsets are those of a whole tile: tokens 16 .. 31 sit at the second page's start
@@ -182,8 +194,8 @@ __device__ __forceinline__ void fetch(uint32_t stage, const Pages<T, D, SMALL>& 
     for (int d = 0; d < DPT; ++d) {
       const int q = wave + NW * d;
       const bool second = to.off[d] >= HALF;
-      dma16((q < R::KBLOCKS ? pages.k : pages.v) + (second ? b - HALF : a) + to.off[d],
-            stage + static_cast<uint32_t>(q) * 1024u);
+      stream16((q < R::KBLOCKS ? pages.k : pages.v) + (second ? b - HALF : a) + to.off[d],
+               stage + static_cast<uint32_t>(q) * 1024u);
     }
   }
 }
@@ -420,7 +432,21 @@ __device__ __forceinline__ int2 page_ids(const PagedAttendParams& p, const Place
   return make_int2(x, SMALL ? table[min(a + 1, last)] : x);
 }
 
-template <typename T, int D, int DEPTH, bool SMALL>
+// Eight elements, with the non-temporal hint or without.
+template <typename T, bool NT>
+__device__ __forceinline__ typename Mfma<T>::Frag load8(const T* p) {
+  if constexpr (!NT) {
+    return Mfma<T>::load(p);
+  } else if constexpr (sizeof(T) == 2) {
+    return __builtin_bit_cast(typename Mfma<T>::Frag, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
+  } else {
+    const f32x4_t a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(p));
+    const f32x4_t b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(p) + 1);
+    return typename Mfma<T>::Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+}
+
+template <typename T, int D, int DEPTH, bool NT, bool SMALL>
 __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece, int g, int lane) {
   using M = Mfma<T>;
   const int lr = lane & 15, lg = lane >> 4;
@@ -468,14 +494,14 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
       int tok = min(ktok + 4 * kb, lim);
       const T* src = base_of(p.k_pages, id, x.tile, tok) + tok * D + 8 * lg;
 #pragma unroll
-      for (int ds = 0; ds < D / 32; ++ds) f.k[kb][ds] = M::load(src + 32 * ds);
+      for (int ds = 0; ds < D / 32; ++ds) f.k[kb][ds] = load8<T, NT>(src + 32 * ds);
     }
   };
   auto load_values = [&](Set& f, const Place& x, int2 id) {
     int tok = 8 * min(lg, (x.len - 1 - 32 * x.tile) >> 3);
     const T* src = base_of(p.v_pages, id, x.tile, tok) + tok * D + 8 * lr;
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) f.v[db] = M::load(src + 128 * db);
+    for (int db = 0; db < D / 16; ++db) f.v[db] = load8<T, NT>(src + 128 * db);
   };
   auto load_rows = [&](Set& f, const Place& x) {
     int i = x.seq - p.B, h = min(lr, p.G - 1);       // a segment's rows are its question's heads
@@ -563,12 +589,13 @@ __device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
          h[8] == p.table_pages << p.page_shift;
 }
 
-#ifndef WDEPTH
-#define WDEPTH 2
-#endif
+// RB = 0: a batch whose prompts have 16 rows at most, and so no block line.  Its
+// contexts stream through the wave line with the non-temporal hint (64 requests
+// of up to 16k tokens 376 -> 357 us); beside a block line the wave line holds
+// segments mostly, and gains nothing by it (4096 x 16: 137 -> 141, eight layers).
 template <typename T, int D, int NW, int NS, int RB, bool SMALL>
 __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendParams p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char ring[NS * Ring<T, D, NS>::STAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RB ? NS * Ring<T, D, NS>::STAGE : 16];
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (!plan_fits(p)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(p.err_flag, kFlagBadLayout);
@@ -576,12 +603,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendPar
   }
   const int n1 = scalars(p.plan)[6], n2 = scalars(p.plan)[7];
   const int g = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv;
-  if (b < n1) {
-    block_piece<T, D, NW, NS, RB, SMALL>(p, ring, b, g, wave, lane);
-    return;
+  if constexpr (RB > 0) {
+    if (b < n1) {
+      block_piece<T, D, NW, NS, RB, SMALL>(p, ring, b, g, wave, lane);
+      return;
+    }
   }
   const int piece = wave * (p.W - n1) + (b - n1);
-  if (piece < n2) wave_piece<T, D, (sizeof(T) * D > 256 ? 1 : WDEPTH), SMALL>(p, piece, g, lane);
+  if (piece < n2) wave_piece<T, D, (sizeof(T) * D > 256 ? 1 : 2), RB == 0, SMALL>(p, piece, g, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -643,7 +672,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttend
         const int k = min(k0 + x * phases, n - 1);
         const int64_t row = base + (k < n0 ? row0 + static_cast<int64_t>(k) * step0 : row1 + static_cast<int64_t>(k - n0) * p.G);
         ml[x] = *reinterpret_cast<const float2*>(p.part_ml + 2 * row);
-        o[x] = *reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d);
+        o[x] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d));
       }
 #pragma unroll
       for (int x = 0; x < BATCH; ++x)
@@ -708,13 +737,16 @@ hipError_t launch(const PagedAttendParams& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_paged_attend(int dtype, int D, int waves, int rb, const PagedAttendParams& p, hipStream_t s) {
-  if (dtype == 0) return D == 64 ? launch<float, 64, 4, 5, 1>(p, s) : launch<float, 128, 8, 4, 1>(p, s);
+  if (dtype == 0) {
+    if (D == 64) return rb == 0 ? launch<float, 64, 4, 5, 0>(p, s) : launch<float, 64, 4, 5, 1>(p, s);
+    return rb == 0 ? launch<float, 128, 8, 4, 0>(p, s) : launch<float, 128, 8, 4, 1>(p, s);
+  }
   if (D == 64) {
     if (waves == 8) return launch<uint16_t, 64, 8, 9, 2>(p, s);
-    return rb == 2 ? launch<uint16_t, 64, 4, 9, 2>(p, s) : launch<uint16_t, 64, 4, 9, 1>(p, s);
+    return rb == 0 ? launch<uint16_t, 64, 4, 9, 0>(p, s) : rb == 1 ? launch<uint16_t, 64, 4, 9, 1>(p, s) : launch<uint16_t, 64, 4, 9, 2>(p, s);
   }
   if (waves == 8) return launch<uint16_t, 128, 8, 9, 2>(p, s);
-  return rb == 2 ? launch<uint16_t, 128, 4, 5, 2>(p, s) : launch<uint16_t, 128, 4, 5, 1>(p, s);
+  return rb == 0 ? launch<uint16_t, 128, 4, 5, 0>(p, s) : rb == 1 ? launch<uint16_t, 128, 4, 5, 1>(p, s) : launch<uint16_t, 128, 4, 5, 2>(p, s);
 }
 
 }  // namespace ippd

@@ -33,7 +33,7 @@ struct PagedShape {
   int G, page_shift;
   int W;                                  // workgroups per kv head
   int waves;                              // waves of a workgroup: 4, two workgroups on a compute unit, or 8
-  int rb;                                 // 16-row blocks per wave of a block-line piece
+  int rb;                                 // 16-row blocks per wave of a block-line piece (0: no block line)
   int group_q;                            // questions of a block-line row group (0: no block line)
   int64_t rows;                           // partial states per kv head
   // word offsets of the plan's arrays

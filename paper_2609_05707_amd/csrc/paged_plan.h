@@ -57,7 +57,7 @@ inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   // rows than four waves hold (a second row group would stream it again), and for
   // fp32 at head_dim 128, whose ring leaves no room for a second workgroup.
   s.waves = (bf16 ? most > 128 : bt->head_dim == 128) ? 8 : 4;
-  s.rb = bf16 && most > 64 ? 2 : 1;
+  s.rb = most <= 16 ? 0 : bf16 && most > 64 ? 2 : 1;
   s.block_cost = bf16 ? 1 : s.waves;
   s.W = std::max(2, kPagedComputeUnits * (s.waves == 8 ? 1 : 2) / bt->num_kv_heads);
   s.group_q = most > 16 ? 16 * s.waves * s.rb / s.G : 0;
