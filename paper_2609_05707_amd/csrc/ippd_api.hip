@@ -398,7 +398,7 @@ ippd_status_t ippd_paged_plan(const ippd_paged_batch_t* bt, void* plan, size_t p
   p.max_len = bt->table_pages * bt->page_tokens;
   p.piece1 = s.piece1; p.piece2 = s.piece2; p.task1 = s.task1; p.task2 = s.task2; p.quest = s.quest;
   p.prompt = s.prompt; p.qlist = s.qlist; p.rank = s.rank; p.where = s.where;
-  p.block_cost = s.block_cost;
+  p.by_rows = s.by_rows; p.wave_shortest = s.wave_shortest;
   return hip_status(ippd::launch_paged_plan(p, stream));
 }
 

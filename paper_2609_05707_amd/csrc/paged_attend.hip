@@ -409,7 +409,7 @@ __device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned
 // the ends of tasks too (a short segment is a tile or two): the page ids run a
 // tile ahead of the loads, the record of the next task a task ahead, all by
 // scalar loads.  Every tile issues the same loads, behind the piece's last tile
-// that one's again: the compiler counts them to know what is still in flight,
+// a token's: the compiler counts them to know what is still in flight,
 // and a load under a condition would make it wait for all.  Loads of a last
 // tile stay within the sequence's tokens, so that a segment costs the bytes it has.
 // ---------------------------------------------------------------------------
@@ -452,7 +452,7 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   const int lr = lane & 15, lg = lane >> 4;
   scalar_words pw = scalars(p.plan + p.piece2 + static_cast<int64_t>(piece) * kPieceWords);
   const int n = pw[2];
-  Place at[DEPTH + 2];                               // of tiles t .. t + DEPTH + 1 (behind the last: that one again)
+  Place at[DEPTH + 2];                               // of tiles t .. t + DEPTH + 1 (behind the last: that one's first token)
   Place after;                                       // the start of the task behind the furthest place's
   at[0].load(p, pw[0]);
   at[0].tile = pw[1];
@@ -460,7 +460,10 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   after.load(p, at[0].index + 1);
   auto follow = [&](const Place& from, int t) {      // the place of tile t, behind `from`
     Place to = from;
-    if (t >= n) return to;
+    if (t >= n) {                                    // its loads are for nothing: one token's
+      to.len = min(to.len, 32 * to.tile + 1);
+      return to;
+    }
     if (++to.tile < to.tiles) return to;
     to = after;
     after.load(p, to.index + 1);

@@ -38,7 +38,8 @@ struct PagedShape {
   int64_t rows;                           // partial states per kv head
   // word offsets of the plan's arrays
   int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank, where, words;
-  int block_cost;                         // a block-line tile's cost to a workgroup, in the wave line's
+  int by_rows;                            // a block-line tile costs by its row blocks (fp32)
+  int wave_shortest;                      // the shortest pieces of the wave line, in tiles
   size_t off_ml, workspace_bytes;
 };
 
@@ -64,7 +65,7 @@ struct PagedPlanParams {
   int B, Nt, G, W, waves, group_q, max_questions;
   int max_len;                            // table_pages * page_tokens
   int64_t piece1, piece2, task1, task2, quest, prompt, qlist, rank, where;
-  int block_cost;
+  int by_rows, wave_shortest;
 };
 
 struct PagedAttendParams {

@@ -58,7 +58,12 @@ inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   // fp32 at head_dim 128, whose ring leaves no room for a second workgroup.
   s.waves = (bf16 ? most > 128 : bt->head_dim == 128) ? 8 : 4;
   s.rb = most <= 16 ? 0 : bf16 && most > 64 ? 2 : 1;
-  s.block_cost = bf16 ? 1 : s.waves;
+  s.by_rows = bf16 ? 0 : 1;
+  // A piece's start against its states in the join: bf16, one request of 8192
+  // tokens 150 us at 2, 131 at 4, 139 at 8 (eight layers), 4096 x 16 136, 133, 133;
+  // an fp32 tile takes a wave longer than a piece's start (256 tokens, 4 questions
+  // 16.0 us at 1, 17.0 at 2).
+  s.wave_shortest = bf16 ? 4 : 1;
   s.W = std::max(2, kPagedComputeUnits * (s.waves == 8 ? 1 : 2) / bt->num_kv_heads);
   s.group_q = most > 16 ? 16 * s.waves * s.rb / s.G : 0;
   const int64_t nt = bt->num_questions, b = bt->num_prompts, w1 = s.W, w2 = w1 * s.waves;

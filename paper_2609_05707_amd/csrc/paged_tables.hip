@@ -414,28 +414,37 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __syncthreads();
 
   // tiles of the two lines
-  int64_t t1 = 0, t2 = 0, T1, T2;
+  int64_t t1 = 0, t2 = 0, T1, T2, c1 = 0, none = 0, C1, zero;
   if (!bad) {
     for (int b = tid; b < B; b += threads) {
       const int n = rank(start(b + 1)) - rank(start(b)), tiles = tiles_of(len(b));
-      if (p.group_q > 0 && n * G > 16) t1 += static_cast<int64_t>((n + p.group_q - 1) / p.group_q) * (tiles > 0 ? tiles + kSetup : 0);
-      else if (n > 0) t2 += tiles;
+      if (p.group_q > 0 && n * G > 16) {
+        const int groups = (n + p.group_q - 1) / p.group_q;
+        const int64_t length = tiles > 0 ? static_cast<int64_t>(groups) * (tiles + kSetup) : 0;
+        t1 += length;
+        c1 += length * (p.by_rows ? max(2, ((n + groups - 1) / groups * G + 15) >> 4) : 2);
+      } else if (n > 0) {
+        t2 += tiles;
+      }
     }
     for (int k = tid; k < nact; k += threads) t2 += tiles_of(len(B + list(k)));
   }
   scan(t1, t2, T1, T2);
-  // workgroups to the lines by their shares of the work, runs of two tiles at
-  // least on the wave line.  Bound by the stream (bf16) a tile costs a workgroup
-  // the same on either line (twice as much on the block line: 8 prompts of 8192
-  // x 32 248 -> 269 us, three layers); bound by the products (fp32) a workgroup
-  // does as many tiles on the wave line as it has waves.
+  scan(c1, none, C1, zero);
+  // workgroups to the lines by their shares of the work, runs of
+  // p.wave_shortest tiles at least on the wave line.  Bound by the stream (bf16) a
+  // tile costs a workgroup the same on either line (twice as much on the block
+  // line: 8 prompts of 8192 x 32 248 -> 269 us, three layers; three quarters
+  // 235).  Bound by the products (fp32) it costs half as much as it has row
+  // blocks: 64 rows of 128-wide heads 96 us at 4 and 67 at 2, 128 rows 172 at 4
+  // and 230 at 2.
   int n1 = 0, n2 = 0;
   if (T1 > 0) {
-    const int64_t most = p.W - (T2 > 0 ? 1 : 0), c1 = T1 * p.block_cost;
-    const int64_t share = quotient(c1 * p.W + (c1 + T2) / 2, c1 + T2);
+    const int64_t most = p.W - (T2 > 0 ? 1 : 0), all = C1 + 2 * T2;
+    const int64_t share = quotient(C1 * p.W + all / 2, all);
     n1 = static_cast<int>(min(max(min(share, T1 / kShortest), static_cast<int64_t>(1)), most));
   }
-  if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(p.waves) * (p.W - n1), (T2 + 1) / 2));
+  if (T2 > 0) n2 = static_cast<int>(min(static_cast<int64_t>(p.waves) * (p.W - n1), (T2 + p.wave_shortest - 1) / p.wave_shortest));
   const Line line1(T1, n1), line2(T2, n2);
 
   // block line: contexts, their active questions in even groups
