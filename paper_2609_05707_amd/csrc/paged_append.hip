@@ -20,7 +20,10 @@ namespace ippd {
 
 namespace {
 
-constexpr int kStepRows = 1024;   // up to so many rows a workgroup takes one row, above them eight
+// Up to so many rows a workgroup takes one row, above them eight.  32 + 8 heads x
+// 128, bf16: 1500 rows without queries 11.2 us by one and 9.1 by eight, with them
+// 14.4 and 18.4, 3000 rows 23.6 and 21.5.
+constexpr int kStepRows = 1024, kStepRowsWithQueries = 2048;
 
 template <typename T> struct Vec16 { static constexpr int N = 16 / static_cast<int>(sizeof(T)); typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
 template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8))); };
@@ -108,12 +111,15 @@ __global__ __launch_bounds__(1024) void append_row_kernel(PagedAppendParams p) {
 // Eight rows a workgroup.  Waves 0 and 1 turn keys, 2 and 3 carry the values,
 // then all turn the queries: lane (row, 8 pairs) evaluates its angles once for
 // all heads.  Values: eight rows in consecutive slots of one 8-token block are
-// transposed in registers into 16-byte pieces (fp32: 32) and written by the
-// workgroup that holds the first of them, so that a fill whose rows do not
-// start on a multiple of eight writes whole blocks too; other rows are written
-// by themselves, element by element.  The inputs are read once and with that hint;
-// the pages are written without it.  30.7k tokens of 8 heads x 128 (252 MB moved),
-// bf16: 67 us with ordinary loads, 60 us (4.2 TB/s) so, 129 with the hint on both.
+// transposed in registers into pieces of a dim's eight tokens, put in order in
+// LDS and written as whole lines, by the workgroup that holds the first of them,
+// so that a fill whose rows do not start on a multiple of eight writes whole
+// blocks too; other rows are written by themselves, element by element.
+//
+// The inputs and the values' lines go with the non-temporal hint, the keys without:
+// 30.7k tokens of 8 heads x 128 (252 MB moved), bf16: 67 us with values in 16-byte
+// pieces (129 with the hint, which then writes parts of lines), 63.5 by whole
+// lines, 55.4 (4.5 TB/s) with the hint on them, 57.9 with it on the keys as well.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   typedef typename Vec8<T>::type vec_t;
@@ -122,6 +128,7 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   const int r0 = blockIdx.x * 8;
   // slots of rows r0 - 7 .. r0 + 14: whether a block is whole takes its rows' all
   __shared__ int near[24];
+  __shared__ vec_t turn_v[2][64 * 8];
   if (threadIdx.x < 22) {
     const int r = r0 - 7 + static_cast<int>(threadIdx.x);
     int slot = r >= 0 && r < p.num_rows ? p.slot_map[r] : -1;
@@ -174,22 +181,35 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
 #pragma unroll
       for (int w = 0; w < 8; ++w) whole = whole && near[l + w] == s - a + w;
       if (whole && a != 0) continue;                 // its first row writes it
-      for (int e = (wave - 2) * 64 + lane; e < p.Hkv * (D / 8); e += 128) {
+      const int items = p.Hkv * (D / 8);
+      for (int e0 = (wave - 2) * 64; e0 < items; e0 += 128) {
+        const int e = min(e0 + lane, items - 1);     // 8 dims of a head
         const int g = e / (D / 8), d0 = (e % (D / 8)) * 8;
         const T* src = v + static_cast<int64_t>(r0 + u) * p.v_stride + g * D + d0;
-        T* dst = vp + value_at(p, s, g) + d0 * 8;
         if (whole) {
           vec_t x[8];
 #pragma unroll
           for (int w = 0; w < 8; ++w) x[w] = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(src + w * p.v_stride));
+          // dim d of item i is piece 8 i + d of the wave's; piece c is at c ^ (c / 8 % 8)
+          vec_t* mine = turn_v[wave - 2];
+          __builtin_amdgcn_wave_barrier();           // (a wave's LDS operations keep their order)
 #pragma unroll
           for (int d = 0; d < 8; ++d) {
             vec_t y;
 #pragma unroll
             for (int w = 0; w < 8; ++w) y[w] = x[w][d];
-            *reinterpret_cast<vec_t*>(dst + d * 8) = y;
+            mine[8 * lane + (d ^ (lane & 7))] = y;
           }
-        } else {
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int c = 64 * k + lane, item = e0 + c / 8;
+            const vec_t y = mine[c ^ (c / 8 % 8)];
+            const int gi = item / (D / 8), di = item % (D / 8) * 8 + c % 8;
+            if (item < items) __builtin_nontemporal_store(y, reinterpret_cast<vec_t*>(vp + value_at(p, s, gi) + di * 8));
+          }
+        } else if (e0 + lane < items) {
+          T* dst = vp + value_at(p, s, g) + d0 * 8;
           const vec_t x = *reinterpret_cast<const vec_t*>(src);
 #pragma unroll
           for (int d = 0; d < 8; ++d) dst[d * 8 + a] = x[d];
@@ -207,7 +227,7 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
 
 template <typename T>
 void launch_append(const PagedAppendParams& p, hipStream_t s) {
-  if (p.num_rows <= kStepRows) {
+  if (p.num_rows <= (p.q ? kStepRowsWithQueries : kStepRows)) {
     constexpr int VE = Vec16<T>::N;
     const int items = ((p.q ? p.Hq : 0) + p.Hkv) * (p.D / 2 / VE) + p.Hkv * (p.D / 2);
     const int threads = std::min(1024, (items + 63) / 64 * 64);

@@ -164,6 +164,20 @@ def test_reserve_bad_layout_moves_nothing(fault, rows):
     assert all(np.array_equal(x, y) for x, y in zip(before, after))
 
 
+@pytest.mark.parametrize("rows", [40, 9000])
+def test_reserve_page_on_the_stack_outside_the_pool(rows):
+    """Its tokens get no slot; the others theirs."""
+    db, st = make([1], (4, 2), 64, "bf16", 16, 8, 8, layers=0)
+    db.free_pages[7] = 8                                    # the first page taken
+    slots, pos, served = (torch.full((m,), 7, dtype=torch.int32, device="cuda") for m in (rows, rows, 2))
+    db.reserve(dev32([20, 3]), dev32([0, 20, 23]), rows, slots, pos, served)
+    assert db.err_flag() == R.BAD
+    want = st.reserve(np.array([20, 3]), np.array([0, 20, 23]), rows)
+    got = slots.cpu().numpy()
+    assert (got[:16] == -1).all() and np.array_equal(got[16:], want[0][16:])
+    assert (pos.cpu().numpy()[:16] == -1).all() and np.array_equal(pos.cpu().numpy()[16:], want[1][16:])
+
+
 # ----------------------------------------------------------------------- append
 def put(kp, vp, slots, k, v, page):
     for row, s in enumerate(slots):
@@ -181,7 +195,8 @@ def half_step(x, bf):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("page,heads,rows,lead,with_q", [
     (16, (4, 2), 1, 0, True), (32, (3, 3), 37, 0, True), (64, (16, 1), 1024, 3, False), (128, (10, 2), 1025, 0, True),
-    (256, (8, 8), 1300, 5, False), (16, (5, 5), 2001, 1, True), (64, (8, 1), 1031, 7, True)])
+    (256, (8, 8), 1300, 5, False), (16, (5, 5), 2001, 1, True), (64, (8, 1), 1031, 7, True), (32, (6, 3), 2049, 0, True),
+    (16, (5, 1), 2051, 6, True), (128, (10, 2), 2103, 3, False)])
 def test_append_against_64_bits(dtype, d, page, heads, rows, lead, with_q):
     """Rows whose slots run over pages from an offset of `lead`, with gaps, single rows out of order and rows without a
     slot; q, k, v as views of one projection with rows further apart than they are long."""
@@ -632,6 +647,75 @@ def test_two_streams_with_workspaces_of_their_own():
                                               qd.data_ptr(), o.data_ptr(), None, w.data_ptr(), db.ws_bytes, s.cuda_stream)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], ref) and torch.equal(outs[1], ref)
+
+
+@pytest.mark.parametrize("page,offset", [(256, 16900), (16, 270000)])
+def test_pages_beyond_32_bits(page, offset):
+    """The same steps in a small pool and in pages of a large one whose offsets pass 32 bits, bit for bit: both append
+    kernels, both lines of the attention."""
+    heads, d, need = (32, 8), 128, 4096 // page
+    lens = np.array([1300, 500, 40, 3, 17, 300])
+    dbs = []
+    for pool, base in ((need, 0), (offset + need, offset)):
+        st = R.State([2, 2], page, need, need)
+        db = PagedBatch([2, 2], heads[0], heads[1], d, "bf16", page, pool, need, rope_base=BASE, layers=1)
+        db.free_pages[:need] = dev32(base + np.arange(need - 1, -1, -1))
+        db.free_count.fill_(need)
+        dbs.append((db, base))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    rows = int(start[-1])
+    fill = torch.randn(rows, 16, d, generator=g, device="cuda").to(torch.bfloat16)
+    x = torch.randn(4, 48, d, generator=g, device="cuda").to(torch.bfloat16)
+    got = []
+    for db, base in dbs:
+        slots, pos = (torch.empty(rows, dtype=torch.int32, device="cuda") for _ in "sp")
+        served = torch.empty(6, dtype=torch.int32, device="cuda")
+        db.reserve(dev32(lens), dev32(start), rows, slots, pos, served)
+        db.append(0, slots, pos, fill[:, :8], fill[:, 8:])
+        db.reserve(dev32([0, 0, 1, 1, 1, 1]), dev32([0, 0, 0, 1, 2, 3, 4]), 4, slots[:4], pos[:4], served)
+        q, k, v = x.split([32, 8, 8], dim=1)
+        q_rot, out, lse = torch.empty(4, 32, d, dtype=torch.bfloat16, device="cuda"), torch.zeros_like(q).contiguous(), \
+            torch.zeros(4, 32, device="cuda")
+        db.append(0, slots[:4], pos[:4], k, v, q, q_rot)
+        db.plan()
+        db.decode(0, q_rot, out, lse)
+        assert db.err_flag() == 0
+        held = int(db.free_count)                            # pages base + held .. base + need - 1 are taken
+        assert int(slots[:4].max()) >= base * page
+        got.append((out, lse, q_rot, slots[:4] - base * page, held))
+    for a, b in zip(*got):
+        assert torch.equal(a, b) if torch.is_tensor(a) else a == b
+    # what of the pages was written agrees too: the tokens of every sequence
+    (small, _), (large, _) = dbs
+    ids = small.block_table.long()
+    for s, n in enumerate(lens + np.array([0, 0, 1, 1, 1, 1])):
+        m = -(-int(n) // page)
+        ks, kl = small.k_pages[0][ids[s, :m]], large.k_pages[0][ids[s, :m] + offset]
+        vs, vl = small.v_pages[0][ids[s, :m]], large.v_pages[0][ids[s, :m] + offset]
+        for a, b, order in ((ks, kl, (0, 2, 1, 3)), (vs, vl, (0, 2, 4, 1, 3))):
+            assert torch.equal(a.permute(order).reshape(m * page, -1)[:n], b.permute(order).reshape(m * page, -1)[:n])
+
+
+def test_calls_go_to_the_current_stream():
+    """A step queued on another stream behind a long kernel there, its inputs written just before."""
+    db, st, q, k, v = filled([6, 2], [120, 40], [9] * 8, (8, 2), 64, "bf16", 16, seed=60)
+    ref, _ = check(db, st, np.ones(8), q, k, v)
+    qd = torch.from_numpy(q).to(db.tdtype).cuda()
+    out, buf = torch.zeros_like(qd), torch.zeros_like(qd)
+    big = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    db.plan_buf.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(5):
+            big = big @ big * 1e-3
+        buf.copy_(qd)
+        db.plan()
+        db.decode(0, buf, out)
+    side.synchronize()
+    assert torch.equal(out, ref)
 
 
 def test_no_questions():
