@@ -585,11 +585,12 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   if (any && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
 
-// Whether the buffer holds a plan of this batch's sizes.
+// Whether the buffer holds a plan of this batch's sizes (no branches: its loads go
+// out together, and with others).
 __device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
   scalar_words h = scalars(p.plan);
-  return h[0] == kPlanMagic && h[1] == p.B && h[2] == p.Nt && h[3] == p.W && h[4] == p.group_q && h[5] == p.G &&
-         h[8] == p.table_pages << p.page_shift;
+  return (h[0] == kPlanMagic) & (h[1] == p.B) & (h[2] == p.Nt) & (h[3] == p.W) & (h[4] == p.group_q) & (h[5] == p.G) &
+         (h[8] == p.table_pages << p.page_shift);
 }
 
 // RB = 0: a batch whose prompts have 16 rows at most, and so no block line.  Its
@@ -617,12 +618,15 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendPar
 }
 
 // ---------------------------------------------------------------------------
-// Join: a unit of one, two or four waves takes a (question, head).  A lane folds
-// every (64 / (D / 4) x waves)-th of the head's states for four dims; lanes of a
-// wave are joined by swaps, waves in LDS.  The plan says how many states the
-// widest question has, and with it how many waves a unit takes: few states and
-// many questions are bound by the states' bytes, one question of many by the
-// latency of a lane's chain.
+// Join: a wave takes a (question, head), or four do where some question has many
+// states.  A lane folds every (64 / (D / 4) x waves)-th of the head's states for
+// four dims; lanes of a wave are joined by swaps, waves in LDS.
+//
+// What bounds it is latency (a question's record, then its states) and, for many
+// questions, the states' bytes.  One wave, its record read with the plan's header:
+// 4096 x 16 (23 states) 134 -> 125 us for eight layers, where two or four waves a
+// unit, known from the header first, took as long; ragged 317, 330 with two, 348
+// with four.  One request of 8192 tokens (65 states) 150 us with one, 134 with four.
 // ---------------------------------------------------------------------------
 constexpr int kJoinWaves = 4;
 
@@ -648,23 +652,30 @@ __device__ __forceinline__ float far32(float x) {
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttendParams p, int units) {
-  constexpr int L = D / 4, IN = 64 / L, BATCH = 4;   // lanes of a state; states a wave reads at once
-  __shared__ float part[kJoinWaves][64][6];
-  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (!plan_fits(p)) return;
-  const int most = scalars(p.plan)[9];               // states of the widest question
-  const int wpu = most <= 2 * BATCH * IN ? 1 : most <= 4 * BATCH * IN ? 2 : 4;
-  const int sub = wave & (wpu - 1), per = kJoinWaves / wpu;
-  const int d = (lane % L) * 4, phase = sub * IN + lane / L, phases = wpu * IN;
-  for (int u0 = blockIdx.x * per; u0 < units; u0 += gridDim.x * per) {
-    const int u = u0 + wave / wpu;
+// A question's record: whether it is served, and where its states are.
+struct Record {
+  int on, row0, n0, step0, row1, n1;
+  __device__ __forceinline__ void load(const PagedAttendParams& p, int unit) {
+    scalar_words w = scalars(p.plan + p.quest + static_cast<int64_t>(min(unit / p.Hq, p.Nt - 1)) * kQuestionWords);
+    on = w[0]; row0 = w[1]; n0 = w[2]; step0 = w[3]; row1 = w[4]; n1 = w[5];
+  }
+};
+
+// Units blockIdx.x * (kJoinWaves / WPU) + .. and on; rec: the first one's record.
+template <typename T, int D, int WPU>
+__device__ __forceinline__ void join_units(const PagedAttendParams& p, int units, Record rec, float (*part)[64][6], int wave,
+                                           int lane) {
+  constexpr int L = D / 4, IN = 64 / L, BATCH = 4, PER = kJoinWaves / WPU;   // lanes of a state; states a lane reads at once
+  const int sub = wave % WPU, d = (lane % L) * 4, phase = sub * IN + lane / L, phases = WPU * IN;
+  const int step = gridDim.x * PER;
+  for (int u0 = blockIdx.x * PER; u0 < units; u0 += step) {
+    const int u = u0 + wave / WPU;
     const int i = u / p.Hq, hq = u - i * p.Hq, g = hq / p.G, h = hq - g * p.G;
-    scalar_words w = scalars(p.plan + p.quest + static_cast<int64_t>(min(i, p.Nt - 1)) * kQuestionWords);
-    const bool served = u < units && w[0] != 0;
-    const int row0 = w[1] + h, step0 = w[3], row1 = w[4] + h, n0 = served ? w[2] : 0, n = served ? n0 + w[5] : 0;
-    const int64_t base = static_cast<int64_t>(g) * p.rows;
+    const Record r = rec;
+    if (u0 + step < units) rec.load(p, u + step);
+    const bool served = (u < units) & (r.on != 0);
+    const int n0 = r.n0, n = served ? n0 + r.n1 : 0;
+    const int64_t base = static_cast<int64_t>(g) * p.rows + h;
     Part a = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     bool bad = false;
     for (int k0 = phase; k0 < n; k0 += phases * BATCH) {
@@ -673,7 +684,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttend
 #pragma unroll
       for (int x = 0; x < BATCH; ++x) {              // all of them in flight; past the last, the last again
         const int k = min(k0 + x * phases, n - 1);
-        const int64_t row = base + (k < n0 ? row0 + static_cast<int64_t>(k) * step0 : row1 + static_cast<int64_t>(k - n0) * p.G);
+        const int64_t row = base + (k < n0 ? r.row0 + static_cast<int64_t>(k) * r.step0 : r.row1 + static_cast<int64_t>(k - n0) * p.G);
         ml[x] = *reinterpret_cast<const float2*>(p.part_ml + 2 * row);
         o[x] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(p.part_o + row * D + d));
       }
@@ -692,7 +703,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttend
       flag = fmaxf(flag, far16(flag));
     }
     join(a, far32(a.m), far32(a.l), f32x4_t{far32(a.o[0]), far32(a.o[1]), far32(a.o[2]), far32(a.o[3])}, p.c);
-    if (wpu > 1) {
+    if constexpr (WPU > 1) {
       __syncthreads();                               // the last unit's parts have been read
       float* mine = part[wave][lane];
       mine[0] = a.m; mine[1] = flag > 0.f ? -1.f : a.l;
@@ -700,7 +711,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttend
       for (int v = 0; v < 4; ++v) mine[2 + v] = a.o[v];
       __syncthreads();
       if (sub == 0)
-        for (int k = 1; k < wpu; ++k) {
+        for (int k = 1; k < WPU; ++k) {
           const float* x = part[wave + k][lane];
           flag = x[1] < 0.f ? 1.f : flag;
           join(a, x[0], x[1], f32x4_t{x[2], x[3], x[4], x[5]}, p.c);
@@ -721,6 +732,23 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttend
       }
       if (p.lse && d == 0) p.lse[at] = a.l == 0.f ? -INFINITY : a.m * p.scale + logf(a.l);
     }
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PagedAttendParams p, int units) {
+  __shared__ float part[kJoinWaves][64][6];
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int most = scalars(p.plan)[9];               // states of the widest question
+  Record rec;
+  rec.load(p, blockIdx.x * kJoinWaves + wave);
+  asm volatile("" : "+s"(rec.on), "+s"(rec.row0));   // (read here, with the header, not where it is used)
+  if (!plan_fits(p)) return;
+  if (most <= 20 * (64 / (D / 4))) {
+    join_units<T, D, 1>(p, units, rec, part, wave, lane);
+  } else {
+    rec.load(p, blockIdx.x);
+    join_units<T, D, kJoinWaves>(p, units, rec, part, wave, lane);
   }
 }
 
