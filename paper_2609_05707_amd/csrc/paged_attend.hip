@@ -374,14 +374,11 @@ __device__ __forceinline__ void stream(const PagedAttendParams& p, unsigned char
 }
 
 template <typename T, int D, int NW, int NS, int RB, bool SMALL>
-__device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned char* ring, int piece, int g, int wave, int lane) {
+__device__ __forceinline__ void block_piece(const PagedAttendParams& p, unsigned char* ring, int piece, int index, int tile,
+                                            int n, Task task, int g, int wave, int lane) {
   TileOffsets<T, D, NW, NS> to;
   to.init(wave, lane);
-  scalar_words pw = scalars(p.plan + p.piece1 + static_cast<int64_t>(piece) * kPieceWords);
   const int tasks = scalars(p.plan)[10];
-  int index = pw[0], tile = pw[1], n = pw[2];
-  Task task;
-  task.load(p.plan, p.task1 + static_cast<int64_t>(index) * kTaskWords);
   while (true) {
     Pages<T, D, SMALL> pages;
     pages.init(p, task.seq, task.len, g);
@@ -454,8 +451,7 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   const int n = pw[2];
   Place at[DEPTH + 2];                               // of tiles t .. t + DEPTH + 1 (behind the last: that one's first token)
   Place after;                                       // the start of the task behind the furthest place's
-  at[0].load(p, pw[0]);
-  at[0].tile = pw[1];
+  at[0] = {pw[4], pw[5], pw[10], pw[0], pw[1]};
   // (the record behind a line's last task is within the plan, and not used)
   after.load(p, at[0].index + 1);
   auto follow = [&](const Place& from, int t) {      // the place of tile t, behind `from`
@@ -601,15 +597,26 @@ template <typename T, int D, int NW, int NS, int RB, bool SMALL>
 __global__ __launch_bounds__(64 * NW, 2) void paged_attend_kernel(PagedAttendParams p) {
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RB ? NS * Ring<T, D, NS>::STAGE : 16];
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv;
+  // a block-line piece's record is read with the header, not behind it
+  int index = 0, tile = 0, n = 0;
+  Task task = {};
+  if constexpr (RB > 0) {
+    scalar_words pw = scalars(p.plan + p.piece1 + static_cast<int64_t>(b) * kPieceWords);
+    index = pw[0];
+    tile = pw[1];
+    n = pw[2];
+    task.load(p.plan, p.piece1 + static_cast<int64_t>(b) * kPieceWords + 4);
+    asm volatile("" : "+s"(index), "+s"(task.seq), "+s"(task.row));
+  }
+  const int n1 = scalars(p.plan)[6], n2 = scalars(p.plan)[7];
   if (!plan_fits(p)) {
     if (blockIdx.x == 0 && threadIdx.x == 0) raise_flag(p.err_flag, kFlagBadLayout);
     return;
   }
-  const int n1 = scalars(p.plan)[6], n2 = scalars(p.plan)[7];
-  const int g = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv;
   if constexpr (RB > 0) {
     if (b < n1) {
-      block_piece<T, D, NW, NS, RB, SMALL>(p, ring, b, g, wave, lane);
+      block_piece<T, D, NW, NS, RB, SMALL>(p, ring, b, index, tile, n, task, g, wave, lane);
       return;
     }
   }

@@ -20,7 +20,8 @@ namespace ippd {
 
 constexpr int kPlanMagic = 0x49504450;    // first word of a plan
 constexpr int kPlanHeader = 64;           // words of its header
-constexpr int kPieceWords = 4;            // first task, first tile within it, tiles (block line: of that task; wave line: in all), 0
+constexpr int kPieceWords = 12;           // first task, first tile within it, tiles (block line: of that task; wave line: in all), 0;
+                                          // that task's record
 constexpr int kTaskWords = 8;             // sequence, tokens, rows, first active question; first state row, first piece, tiles,
                                           // tiles in the first piece (block line)
 constexpr int kQuestionWords = 8;         // served, context state row, states, rows a state; segment state row, states; 0, 0

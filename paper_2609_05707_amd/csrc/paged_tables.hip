@@ -352,12 +352,15 @@ __device__ __forceinline__ void write_task(int32_t* plan, int64_t tasks, int64_t
   const int64_t tile0 = at + (BLOCK ? kSetup : 0);
   auto until = [&](int p) { return static_cast<int>(min(line.start(p + 1) - tile0, static_cast<int64_t>(tiles))); };
   int4* t = reinterpret_cast<int4*>(plan + tasks + static_cast<int64_t>(index) * kTaskWords);
-  t[0] = make_int4(seq, len, rows, q);
-  t[1] = make_int4(row, first, tiles, BLOCK ? until(first) : 0);
+  const int4 t0 = make_int4(seq, len, rows, q), t1 = make_int4(row, first, tiles, BLOCK ? until(first) : 0);
+  t[0] = t0;
+  t[1] = t1;
   for (int p = line.start(first) >= at ? first : first + 1; p < first + states; ++p) {
     const int tile = static_cast<int>(max(line.start(p) - tile0, static_cast<int64_t>(0)));
-    *reinterpret_cast<int4*>(plan + pieces + static_cast<int64_t>(p) * kPieceWords) =
-        make_int4(index, tile, BLOCK ? until(p) - tile : static_cast<int>(line.start(p + 1) - line.start(p)), 0);
+    int4* rec = reinterpret_cast<int4*>(plan + pieces + static_cast<int64_t>(p) * kPieceWords);
+    rec[0] = make_int4(index, tile, BLOCK ? until(p) - tile : static_cast<int>(line.start(p + 1) - line.start(p)), 0);
+    rec[1] = t0;
+    rec[2] = t1;
   }
 }
 
