@@ -459,8 +459,8 @@ ippd_status_t ippd_paged_reserve(const ippd_paged_batch_t *batch, const int32_t 
  * bytes), so views of one joint projection do.  q_rot [num_rows][Hq][D] is
  * contiguous and overlaps no input.  Rows with slot -1 are not written; a slot
  * outside the pool sets IPPD_FLAG_BAD_LAYOUT and its row is skipped.  The slots
- * of a call are distinct; if one occurs twice, which of its rows' values it
- * keeps is not defined.
+ * of a call are distinct; if one occurs twice, what it holds afterwards is not
+ * defined (any of its rows' elements).
  */
 ippd_status_t ippd_paged_append(const ippd_paged_batch_t *batch, const ippd_pages_t *pages, int32_t num_rows,
                                 const int32_t *slot_map, const int32_t *positions, const void *q, int64_t q_stride,

@@ -2,8 +2,9 @@
 
 The compute lives in libippd.so (hand-written HIP, C ABI in include/ippd.h);
 ``_lib`` is its ctypes binding, ``session.DecodeBatch`` a torch-side holder of
-device buffers and ``paged.PagedBatch`` the same over a paged cache.  Importing this package does not load the library;
-``load_library()`` does, and raises if it has not been built.
+device buffers and ``paged.PagedBatch`` the same over a paged cache.  Importing
+this package does not load the library; ``load_library()`` does, and raises if
+it has not been built.
 """
 from ._lib import (  # noqa: F401
     EXPORTED,

@@ -429,7 +429,7 @@ ippd_status_t ippd_paged_decode_attention(const ippd_paged_batch_t* bt, const ip
   p.rows = s.rows;
   p.piece1 = s.piece1; p.piece2 = s.piece2; p.task1 = s.task1; p.task2 = s.task2; p.quest = s.quest; p.qlist = s.qlist;
   p.B = bt->num_prompts; p.Nt = bt->num_questions; p.Hq = bt->num_q_heads; p.Hkv = bt->num_kv_heads; p.G = s.G;
-  p.W = s.W; p.group_q = s.group_q; p.page_shift = s.page_shift; p.num_pages = bt->num_pages;
+  p.W = s.W; p.waves = s.waves; p.group_q = s.group_q; p.page_shift = s.page_shift; p.num_pages = bt->num_pages;
   p.table_pages = bt->table_pages;
   p.scale = softmax_scale(bt);
   p.c = p.scale * 1.4426950408889634f;

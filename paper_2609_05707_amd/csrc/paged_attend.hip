@@ -581,12 +581,12 @@ __device__ __forceinline__ void wave_piece(const PagedAttendParams& p, int piece
   if (any && lane == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }
 
-// Whether the buffer holds a plan of this batch's sizes (no branches: its loads go
-// out together, and with others).
+// Whether the buffer holds a plan of this batch's sizes, those that its arrays'
+// places follow from (no branches: its loads go out together, and with others).
 __device__ __forceinline__ bool plan_fits(const PagedAttendParams& p) {
   scalar_words h = scalars(p.plan);
   return (h[0] == kPlanMagic) & (h[1] == p.B) & (h[2] == p.Nt) & (h[3] == p.W) & (h[4] == p.group_q) & (h[5] == p.G) &
-         (h[8] == p.table_pages << p.page_shift);
+         (h[8] == p.table_pages << p.page_shift) & (h[11] == p.waves);
 }
 
 // RB = 0: a batch whose prompts have 16 rows at most, and so no block line.  Its

@@ -75,7 +75,7 @@ struct PagedAttendParams {
   void* out; float* lse; float* part_o; float* part_ml; int32_t* err_flag;
   int64_t rows;                           // partial states per kv head
   int64_t piece1, piece2, task1, task2, quest, qlist;
-  int B, Nt, Hq, Hkv, G, W, group_q, page_shift, num_pages, table_pages;
+  int B, Nt, Hq, Hkv, G, W, waves, group_q, page_shift, num_pages, table_pages;
   float c;                                // scale * log2(e)
   float scale;
 };

@@ -3,8 +3,8 @@
 //
 // Both are a few thousand integers, so what bounds them is latency: the
 // dependent round trips to memory and the barriers of a scan.  One workgroup
-// of 1024 threads does a call; only a slot map of many rows gets a launch of
-// its own.
+// does a call, with as many threads as it has sequences or rows (1024 at most);
+// only a slot map of many rows gets a launch of its own.
 #include "ippd_device.h"
 #include "paged_internal.h"
 
@@ -575,7 +575,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     int4* head = reinterpret_cast<int4*>(plan);
     head[0] = make_int4(kPlanMagic, B, Nt, p.W);
     head[1] = make_int4(p.group_q, G, n1, n2);
-    head[2] = make_int4(p.max_len, widest, block_tasks, 0);
+    head[2] = make_int4(p.max_len, widest, block_tasks, p.waves);
   }
   if (bad && tid == 0) raise_flag(p.err_flag, kFlagBadLayout);
 }

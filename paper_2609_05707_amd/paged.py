@@ -11,6 +11,10 @@ A decode step of a model, with one row per question:
     for layer in range(layers):                              # q, k, v: views of the layer's projection
         db.append(layer, slots, positions, k, v, q, q_rot)
         db.decode(layer, q_rot, out, lse)
+
+Calls on one PagedBatch follow each other on one stream: they share its tables,
+plan and workspace.  Its decode calls on two streams at once need the C entry
+points, with a workspace each.
 """
 from __future__ import annotations
 

@@ -478,6 +478,24 @@ def test_attention_refuses_other_plans():
         assert db.err_flag() == R.BAD and (out == 5.0).all()
 
 
+@pytest.mark.parametrize("most", [1, 20])
+def test_attention_refuses_plans_of_other_workgroups(most):
+    """With 256 kv heads an fp32 and a bf16 batch agree in everything but the waves of a workgroup, and
+    with them in where the plan's arrays lie."""
+    kw = dict(hq=1024, hkv=256, head_dim=128, page_tokens=16, num_pages=8, table_pages=4, layers=1)
+    f = PagedBatch([most], dtype="f32", **kw)
+    b = PagedBatch([most], dtype="bf16", **kw)
+    assert f.plan_bytes != b.plan_bytes
+    plan = torch.zeros(max(f.plan_bytes, b.plan_bytes), dtype=torch.uint8, device="cuda")
+    L.ippd_paged_plan(f.batch, plan.data_ptr(), plan.numel(), torch.cuda.current_stream().cuda_stream)
+    q = torch.zeros(most, 1024, 128, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    L.ippd_paged_decode_attention(b.batch, b.pages[0], plan.data_ptr(), plan.numel(), q.data_ptr(), out.data_ptr(), None,
+                                  b.ws.data_ptr(), b.ws_bytes, torch.cuda.current_stream().cuda_stream)
+    assert b.err_flag() == L.IPPD_FLAG_BAD_LAYOUT and f.err_flag() == 0
+    assert bool((out == 7.0).all())
+
+
 @pytest.mark.parametrize("fault", ["length", "negative", "questions", "csr"])
 def test_plan_bad_layout_serves_nothing(fault):
     db, st, q, k, v = filled([3, 1], [40, 20], [3, 4, 5, 6], (4, 2), 64, "bf16", 16, seed=16)
