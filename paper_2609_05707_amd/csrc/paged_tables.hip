@@ -52,6 +52,20 @@ __device__ __forceinline__ V row_inclusive(V v) {
   v += dpp<0x118, 0xF>(v);
   return v;
 }
+// The same with the largest value in place of the sum, none of them negative.
+__device__ __forceinline__ int row_max(int v) {
+  v = max(v, dpp<0x111, 0xF>(v));
+  v = max(v, dpp<0x112, 0xF>(v));
+  v = max(v, dpp<0x114, 0xF>(v));
+  v = max(v, dpp<0x118, 0xF>(v));
+  return v;
+}
+__device__ __forceinline__ int wave_max(int v) {
+  v = row_max(v);
+  v = max(v, dpp<0x142, 0xA>(v));
+  v = max(v, dpp<0x143, 0xC>(v));
+  return v;
+}
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
   const uint32_t lo = lane_value(static_cast<int>(v), lane), hi = lane_value(static_cast<int>(v >> 32), lane);
@@ -96,6 +110,16 @@ struct Scan {
     __syncthreads();
     return place(inc, 0, at, total) - v;
   }
+  // The largest of the threads' values before this one's (none negative).
+  __device__ __forceinline__ int latest(int v) {
+    const int inc = wave_max(v), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t (*at)[2] = lds[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) at[threadIdx.x >> 6][0] = inc;
+    __syncthreads();
+    const int up = row_max(static_cast<int>(at[threadIdx.x & 15][0]));
+    return max(dpp<0x138, 0xF>(inc), wave ? lane_value(up, wave - 1) : 0);
+  }
 };
 static_assert(kWaves == 16, "the waves' sums are added up in a row of lanes");
 
@@ -108,6 +132,52 @@ __device__ __forceinline__ int last_at_most(const A& a, int n, int x) {
     if (a[mid] <= x) lo = mid; else hi = mid - 1;
   }
   return lo;
+}
+
+// put(k, w, get(k, w)) for every k < total, where w is the sequence of this window
+// that page k falls to: thread t's has the pages ex .. ex + n - 1.  first: ex of
+// each, in LDS (a barrier lies behind it).  Few pages find theirs by a search each;
+// of more a thread takes kPer in a row, and the sequence of a page is the last that
+// marked one up to it.  Some 6k pages of 608 sequences: 10.9 us
+// a call with a search and a round trip each, 9.5 (14.1 with four searches at once:
+// the searches' instructions are what costs).
+constexpr int kPer = 4;
+static_assert(kThreads <= 1 << 16, "a mark has 16 bits");
+template <typename G, typename P>
+__device__ __forceinline__ void move_pages(Scan& scan, uint16_t* marks, const int* first, int sequences, int ex, int n,
+                                           int total, G get, P put) {
+  const int tid = threadIdx.x, threads = blockDim.x;
+  if (total <= threads) {
+    if (tid < total) {
+      const int w = last_at_most(first, sequences, tid);
+      put(tid, w, get(tid, w));
+    }
+    return;
+  }
+  for (int k0 = 0; k0 < total; k0 += kPer * threads) {
+    uint64_t mine = 0;
+    __builtin_memcpy(marks + kPer * tid, &mine, sizeof mine);
+    __syncthreads();
+    if (n > 0 && ex < k0 + kPer * threads && ex + n > k0) marks[max(ex, k0) - k0] = static_cast<uint16_t>(tid);
+    __syncthreads();
+    __builtin_memcpy(&mine, marks + kPer * tid, sizeof mine);
+    int w[kPer], v[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int x = static_cast<int>(mine >> (16 * u)) & 0xFFFF;
+      w[u] = u ? max(w[u - 1], x) : x;
+    }
+    const int before = scan.latest(w[kPer - 1]), k = k0 + kPer * tid;
+    if (k >= total) continue;                        // (uniform barriers: the loop's count is the workgroup's)
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      w[u] = max(w[u], before);
+      v[u] = get(min(k + u, total - 1), w[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (k + u < total) put(k + u, w[u], v[u]);
+  }
 }
 
 __device__ __forceinline__ int pages_of(int tokens, int shift) { return static_cast<int>((static_cast<uint32_t>(tokens) + (1u << shift) - 1u) >> shift); }
@@ -123,9 +193,9 @@ __device__ __forceinline__ int pages_of(int tokens, int shift) { return static_c
 //                     served if the pages needed up to and including its own
 //                     number f' at most (or it needs none).
 // The orders make a shrink the inverse of the growth before it.  Each is a
-// prefix sum over the sequences and then a flat loop over the pages, a thread
-// per page, which finds its sequence by a search of the sums: 32 contexts of
-// 256 pages cost as many rounds as 8192 sequences of one.
+// prefix sum over the sequences and then a flat loop over the pages
+// (move_pages): 32 contexts of 256 pages cost as many rounds as 8192 sequences
+// of one.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void write_row(const ReserveParams& p, int row, int s, int j, int got, int after, int base) {
   int slot = -1, pos = -1;
@@ -148,6 +218,7 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
   __shared__ int64_t sums[2][kWaves][2];
   __shared__ int first[kThreads];                    // pages before the sequence, in this window
   __shared__ int from[kThreads];                     // its first page moved
+  __shared__ __attribute__((aligned(8))) uint16_t marks[kPer * kThreads];   // the sequence whose pages begin at a page
   __shared__ int taken;
   __shared__ int row0[ROWS ? kFusedSequences : 1], after[ROWS ? kFusedSequences : 1], got[ROWS ? kFusedSequences : 1];
   __shared__ int q0[ROWS ? kFusedSequences : 1];
@@ -207,11 +278,11 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
       first[tid] = ex;
       from[tid] = keep;
       __syncthreads();
-      for (int k = tid; k < total; k += threads) {
-        const int w = last_at_most(first, min(threads, S - s0), k);
-        const int64_t row = static_cast<int64_t>(s0 + w) * p.table_pages;
-        p.free_pages[f1 - 1 - (carry + k)] = p.block_table[row + from[w] + (k - first[w])];
-      }
+      move_pages(scan, marks, first, min(threads, S - s0), ex, n, total,
+                 [&](int k, int w) {
+                   return p.block_table[static_cast<int64_t>(s0 + w) * p.table_pages + from[w] + (k - first[w])];
+                 },
+                 [&](int k, int, int page) { p.free_pages[f1 - 1 - (carry + k)] = page; });
       carry += total;
     }
   }
@@ -266,11 +337,11 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
     __syncthreads();
     // the served sequences are those of a leading run of the pages needed
     const int run = min(total, taken - carry);
-    for (int k = tid; k < run; k += threads) {
-      const int w = last_at_most(first, min(threads, S - s0), k);
-      const int64_t row = static_cast<int64_t>(s0 + w) * p.table_pages;
-      p.block_table[row + from[w] + (k - first[w])] = p.free_pages[f1 - 1 - (carry + k)];
-    }
+    move_pages(scan, marks, first, min(threads, S - s0), ex, need, run,
+               [&](int k, int) { return p.free_pages[f1 - 1 - (carry + k)]; },
+               [&](int k, int w, int page) {
+                 p.block_table[static_cast<int64_t>(s0 + w) * p.table_pages + from[w] + (k - first[w])] = page;
+               });
     carry += total;
   }
   __syncthreads();                                   // tables, and the page count
@@ -286,15 +357,26 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
 }
 
 // The slot map of many rows, a thread per row; the reservation's kernel has
-// left the lengths after it and what each sequence was served.
+// left the lengths after it and what each sequence was served.  Up to
+// kFusedSequences the offsets are searched in LDS, a round trip to memory and not
+// one a step.
+template <bool LDS>
 __global__ __launch_bounds__(256) void rows_kernel(ReserveParams p) {
-  const int r = blockIdx.x * 256 + threadIdx.x;
+  __shared__ int row_l[LDS ? kFusedSequences : 1], q_l[LDS ? kFusedSequences : 1];
+  const int S = p.B + p.Nt, r = blockIdx.x * 256 + threadIdx.x;
+  if constexpr (LDS) {
+    for (int i = threadIdx.x; i < S; i += 256) row_l[i] = p.token_start[i];
+    for (int i = threadIdx.x; i < p.B; i += 256) q_l[i] = p.q_start[i];
+    __syncthreads();
+  }
   if (r >= p.num_rows) return;
-  const int s = last_at_most(p.token_start, p.B + p.Nt, r);
+  const int* row0 = LDS ? row_l : p.token_start;
+  const int* q0 = LDS ? q_l : p.q_start;
+  const int s = last_at_most(row0, S, r);
   const int got = max(p.served[s], 0);
   int base = 0;
-  if (s >= p.B) base = p.seq_len[last_at_most(p.q_start, p.B, s - p.B)];
-  write_row(p, r, s, r - p.token_start[s], got, p.seq_len[s], base);
+  if (s >= p.B) base = p.seq_len[last_at_most(q0, p.B, s - p.B)];
+  write_row(p, r, s, r - row0[s], got, p.seq_len[s], base);
 }
 
 // ---------------------------------------------------------------------------
@@ -596,7 +678,9 @@ hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s) {
   reserve_kernel<false><<<1, kThreads, 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.num_rows == 0) return e;
-  rows_kernel<<<static_cast<unsigned>((static_cast<int64_t>(p.num_rows) + 255) / 256), 256, 0, s>>>(p);
+  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.num_rows) + 255) / 256);
+  if (sequences <= kFusedSequences) rows_kernel<true><<<grid, 256, 0, s>>>(p);
+  else rows_kernel<false><<<grid, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

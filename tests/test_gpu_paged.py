@@ -120,6 +120,27 @@ def test_reserve_many_sequences():
     reserve(db, st, mixed, start, int(start[-1]))
 
 
+@pytest.mark.parametrize("prompts,pages", [(3, 700), (3, 9001), (70, 9001), (900, 9001)])
+def test_reserve_many_pages(prompts, pages):
+    """More pages in a call than threads, and than one round of them moves; some prompts get none, some give
+    back a part; the last that asks for more than is left gets nothing."""
+    r = np.random.default_rng(prompts + pages)
+    db, st = make([0] * prompts, (4, 2), 64, "bf16", 16, pages, pages, seed=pages, layers=0)
+    share = np.sort(r.integers(0, pages - 1, size=prompts - 1))
+    new = 16 * np.diff(np.concatenate([[0], share, [pages]])) - r.integers(0, 16, size=prompts)
+    new = np.maximum(new, 0)
+    new[r.integers(0, prompts, size=prompts // 4)] = 0
+    start = np.concatenate([[0], np.cumsum(new)])
+    reserve(db, st, new, start, int(start[-1]))
+    reserve(db, st, -r.integers(0, 16 * pages // prompts, size=prompts), np.zeros(prompts + 1), 0)
+    new = r.integers(0, 40, size=prompts)
+    new[-1] = 16 * pages
+    start = np.concatenate([[0], np.cumsum(new)])
+    reserve(db, st, new, start, int(start[-1]))
+    reserve(db, st, -st.seq_len, np.zeros(prompts + 1), 0)
+    assert st.count == pages
+
+
 def test_reserve_refuses_what_does_not_fit():
     """A full row, an exhausted stack (and later sequences that need no page), all or nothing per sequence."""
     db, st = make([3], (4, 2), 64, "bf16", 16, 6, 4, layers=0)
