@@ -138,9 +138,9 @@ __device__ __forceinline__ int last_at_most(const A& a, int n, int x) {
 // that page k falls to: thread t's has the pages ex .. ex + n - 1.  first: ex of
 // each, in LDS (a barrier lies behind it).  Few pages find theirs by a search each;
 // of more a thread takes kPer in a row, and the sequence of a page is the last that
-// marked one up to it.  Some 6k pages of 608 sequences: 10.9 us
-// a call with a search and a round trip each, 9.5 (14.1 with four searches at once:
-// the searches' instructions are what costs).
+// marked one up to it.  Some 6k pages of 608 sequences take
+// 7.8 us a call, 1.4 more with a search and a round trip each (6 more with four
+// searches at once: the searches' instructions are what costs).
 constexpr int kPer = 4;
 static_assert(kThreads <= 1 << 16, "a mark has 16 bits");
 template <typename G, typename P>
@@ -315,12 +315,13 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
     const bool ok = fits && (need == 0 || upto <= f1);
     first[tid] = ex;
     from[tid] = have;
+    const int most = wave_max(ok && need > 0 ? upto : 0);
+    if ((tid & 63) == 63) atomicMax(&taken, most);
     if (s < S) {
       int now = len, moved = 0;
       if (ok) {
         now = len + c;
         moved = c;
-        if (need > 0) atomicMax(&taken, upto);
       } else if (c > 0 && fits) {
         raise_flag(p.err_flag, kFlagPagesExhausted);
       } else if (c < 0) {
@@ -400,49 +401,84 @@ constexpr int kSetup = 4;
 constexpr int kShortest = 6;
 static_assert(kShortest > kSetup, "a piece may not lie between two tasks' tiles");
 
+// a / b for 0 <= a < 2^52, 0 < b.  The double nearest a / b is on the quotient's side
+// of the next integer: a / b lies 1 / b below it at least, which is 1 / a of it.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  const uint64_t x = a, y = b;
-  if (((x | y) >> 32) == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(y);
-  return static_cast<int64_t>(x / y);
+  return static_cast<int64_t>(static_cast<double>(a) / static_cast<double>(b));
 }
 
 // A line of T tiles cut into n <= T pieces, the first T % n of them one tile longer.
 struct Line {
   int64_t size, longer, edge;                        // tiles of a short piece; pieces that are longer, and where they end
+  double per, per1;                                  // 1 / size, 1 / (size + 1)
   int n;
-  __device__ __forceinline__ Line(int64_t tiles, int pieces) : size(0), longer(0), edge(0), n(pieces) {
-    if (pieces == 0) return;
-    size = quotient(tiles, pieces);
+  __device__ __forceinline__ Line(int64_t tiles, int pieces) : n(pieces) {
+    size = quotient(tiles, max(pieces, 1));
     longer = tiles - size * pieces;
     edge = longer * (size + 1);
+    per = 1.0 / static_cast<double>(size);
+    per1 = 1.0 / static_cast<double>(size + 1);
   }
   __device__ __forceinline__ int64_t start(int p) const { return p * size + (p < longer ? p : longer); }
+  // The piece that place x lies in: the product is within one of it.
   __device__ __forceinline__ int piece_of(int64_t x) const {
-    return static_cast<int>(x < edge ? quotient(x, size + 1) : longer + quotient(x - edge, size));
+    const bool low = x < edge;
+    const int64_t a = low ? x : x - edge, d = low ? size + 1 : size;
+    const int q = static_cast<int>(static_cast<double>(a) * (low ? per1 : per));
+    const int64_t r = a - q * d;
+    return q + (r >= d) - (r < 0) + (low ? 0 : static_cast<int>(longer));
   }
 };
 
-// A task whose `tiles` > 0 tiles follow `setup` places from `at` on the line, in
-// pieces first .. first + states - 1: its record, and the records of the pieces
-// whose first tile is one of its.  A piece ends with its own places: its record
-// counts its tiles on the block line within that task (the next task's record
-// says how many of its tiles are still in the piece), on the wave line in all.
+// The records of the pieces p, p + by, .. < end whose first tile is one of a task's.
+// A piece ends with its own places: its record counts its tiles on the block line
+// within that task (the next task's record says how many of its tiles are still in
+// the piece), on the wave line in all.
 template <bool BLOCK>
-__device__ __forceinline__ void write_task(int32_t* plan, int64_t tasks, int64_t pieces, const Line& line, int index,
-                                           int64_t at, int tiles, int seq, int len, int rows, int q, int row, int first,
-                                           int states) {
-  const int64_t tile0 = at + (BLOCK ? kSetup : 0);
-  auto until = [&](int p) { return static_cast<int>(min(line.start(p + 1) - tile0, static_cast<int64_t>(tiles))); };
-  int4* t = reinterpret_cast<int4*>(plan + tasks + static_cast<int64_t>(index) * kTaskWords);
-  const int4 t0 = make_int4(seq, len, rows, q), t1 = make_int4(row, first, tiles, BLOCK ? until(first) : 0);
-  t[0] = t0;
-  t[1] = t1;
-  for (int p = line.start(first) >= at ? first : first + 1; p < first + states; ++p) {
-    const int tile = static_cast<int>(max(line.start(p) - tile0, static_cast<int64_t>(0)));
+__device__ __forceinline__ void write_pieces(int32_t* plan, int64_t pieces, const Line& line, int index, int64_t tile0,
+                                             int tiles, const int4& t0, const int4& t1, int p, int end, int by) {
+  for (; p < end; p += by) {
+    // places from the task's first tile on (a piece that begins before the task: from less than its setup's)
+    const int64_t from = line.start(p) - tile0, to = from + line.size + (p < line.longer);
+    if (from < (BLOCK ? -kSetup : 0)) continue;
+    const int tile = static_cast<int>(max(from, static_cast<int64_t>(0)));
     int4* rec = reinterpret_cast<int4*>(plan + pieces + static_cast<int64_t>(p) * kPieceWords);
-    rec[0] = make_int4(index, tile, BLOCK ? until(p) - tile : static_cast<int>(line.start(p + 1) - line.start(p)), 0);
+    rec[0] = make_int4(index, tile, static_cast<int>(BLOCK ? min(to, static_cast<int64_t>(tiles)) - tile : to - from), 0);
     rec[1] = t0;
     rec[2] = t1;
+  }
+}
+
+// A lane's task (has: it has one), whose `tiles` > 0 tiles follow `setup` places
+// from `at` on the line, in pieces first .. first + states - 1: its record and its
+// pieces'.  All lanes of a wave are here: one or two tasks of many pieces have theirs
+// written by the whole wave, some 700 cycles each, where a lane takes 300 a record
+// (one prompt of 4096 x 16, 22 pieces: 9300 cycles for the block line, 4900 so; 8
+// tasks of 8 pieces 6200, 10000 so).
+template <bool BLOCK>
+__device__ __forceinline__ void write_task(int32_t* plan, int64_t tasks, int64_t pieces, const Line& line, bool has,
+                                           int index, int64_t at, int tiles, int seq, int len, int rows, int q, int row,
+                                           int first, int states) {
+  constexpr int kWide = 6, kFew = 2;
+  const int64_t tile0 = at + (BLOCK ? kSetup : 0);
+  const int lead = BLOCK ? static_cast<int>(min(line.start(first + 1) - tile0, static_cast<int64_t>(tiles))) : 0;
+  const int4 t0 = make_int4(seq, len, rows, q), t1 = make_int4(row, first, tiles, lead);
+  if (has) {
+    int4* t = reinterpret_cast<int4*>(plan + tasks + static_cast<int64_t>(index) * kTaskWords);
+    t[0] = t0;
+    t[1] = t1;
+  }
+  uint64_t wide = __ballot(has && states > kWide);
+  if (__popcll(wide) > kFew) wide = 0;
+  if (has && !(wide >> (threadIdx.x & 63) & 1))
+    write_pieces<BLOCK>(plan, pieces, line, index, tile0, tiles, t0, t1, first, first + states, 1);
+  while (wide) {
+    const int l = __builtin_ctzll(wide);
+    wide &= wide - 1;
+    auto of = [&](auto v) { return lane_value(v, l); };
+    const int p = of(first);
+    write_pieces<BLOCK>(plan, pieces, line, of(index), of(tile0), of(tiles), make_int4(of(seq), of(len), of(rows), of(q)),
+                        make_int4(of(row), p, of(tiles), of(lead)), p + static_cast<int>(threadIdx.x & 63), p + of(states), 64);
   }
 }
 
@@ -562,14 +598,17 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     }
     int nrow;
     int row = rows + scan(need, nrow);
-    for (int j = 0; j < groups; ++j) {
-      const int64_t x = at0 + static_cast<int64_t>(j) * (tiles + kSetup);
+    for (int j = 0; wave_any(j < groups); ++j) {
+      const bool has = j < groups;
+      const int64_t x = has ? at0 + static_cast<int64_t>(j) * (tiles + kSetup) : 0;
       const int gr = min(per, n - j * per) * G, first = line1.piece_of(x + kSetup);
       const int states = line1.piece_of(x + kSetup + tiles - 1) - first + 1;
       const int t = static_cast<int>(task0) + j;
-      write_task<true>(plan, p.task1, p.piece1, line1, t, x, tiles, b, tokens, gr, r0 + j * per, row, first, states);
-      (LDS ? where_l[t] : where[t]) = make_int2(row, states);
-      row += states * gr;
+      write_task<true>(plan, p.task1, p.piece1, line1, has, t, x, tiles, b, tokens, gr, r0 + j * per, row, first, states);
+      if (has) {
+        (LDS ? where_l[t] : where[t]) = make_int2(row, states);
+        row += states * gr;
+      }
     }
     if (b < B) prompt(b) = make_int4(kind, static_cast<int>(task0), per, r0);
     tasks += ntask;
@@ -606,8 +645,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     const int first = tiles > 0 ? line2.piece_of(at0) : 0, np = tiles > 0 ? line2.piece_of(at0 + tiles - 1) - first + 1 : 0;
     int nrow;
     const int row = rows + scan(np * n, nrow);
-    if (tiles > 0)
-      write_task<false>(plan, p.task2, p.piece2, line2, static_cast<int>(task), at0, tiles, seq, tokens, n, q, row, first, np);
+    write_task<false>(plan, p.task2, p.piece2, line2, tiles > 0, static_cast<int>(task), at0, tiles, seq, tokens, n, q, row, first,
+                      np);
     if (x < B) {
       if (seq >= 0) {
         prompt(x).y = row;
@@ -651,7 +690,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     }
     *reinterpret_cast<int4*>(plan + p.quest + static_cast<int64_t>(i) * kQuestionWords) = rec;
   }
-  if (most > 0) atomicMax(&widest, most);
+  most = wave_max(most);                             // (a lane's atomic each: 64 questions 5000 cycles)
+  if ((tid & 63) == 63) atomicMax(&widest, most);
   __syncthreads();
   if (tid == 0) {
     int4* head = reinterpret_cast<int4*>(plan);
