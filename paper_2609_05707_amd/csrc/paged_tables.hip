@@ -706,7 +706,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
 
 // Threads for n items: whole waves, kThreads at most.  These kernels are bound
 // by latency and, where waves share a SIMD, by the instructions of all of them,
-// so that idle waves cost: plan of 264 sequences 10.5 us with 1024 threads.
+// so that idle waves cost: a plan of 5 to 264 sequences 3.5 to 4 us with 1024 threads.
 static int threads_for(int64_t n) { return static_cast<int>(n >= kThreads ? kThreads : n <= 64 ? 64 : (n + 63) / 64 * 64); }
 
 hipError_t launch_paged_reserve(const ReserveParams& p, hipStream_t s) {
