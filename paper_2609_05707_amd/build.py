@@ -18,7 +18,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(HERE, "libippd.so")
 
 SOURCES = ["ippd_api.hip", "rope_append.hip", "decode_step.hip", "prefill.hip", "dense_mask.hip",
-           "paged_tables.hip", "paged_append.hip", "paged_attend.hip"]
+           "paged_api.hip", "paged_tables.hip", "paged_append.hip", "paged_attend.hip"]
 # standalone measurement programs, built next to the library
 TOOLS = {"stream_ceiling.hip": os.path.join(HERE, "stream_ceiling"), "l2_handoff.hip": os.path.join(HERE, "l2_handoff")}
 ARCH = "gfx950"

@@ -152,6 +152,9 @@ struct StepParams {
   double inv_freq[kMaxHalfDim];
 };
 
+// what ippd_last_hip_error returns on this thread
+void keep_hip_error(hipError_t e);
+
 hipError_t launch_load_context(int dtype, const LoadContextParams& p, hipStream_t s);
 hipError_t launch_load_segments(int dtype, const LoadSegmentsParams& p, hipStream_t s);
 hipError_t launch_append(int dtype, const AppendParams& p, hipStream_t s);

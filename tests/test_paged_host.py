@@ -208,6 +208,18 @@ int main(void) {
 def test_host_code_under_sanitizers(tmp_path, monkeypatch):
     other = pytest.importorskip("tests.test_host_sanitizers")
     monkeypatch.setattr(other, "C_SOURCE", SANITIZED)
+    # the same program with the paged cache's host code built for them, the other objects as they are
+    objects = tmp_path / "objects"
+    objects.mkdir()
+    for o in os.listdir(B.BUILD_DIR):
+        if o.endswith(".o") and o != "paged_api.o":
+            os.symlink(os.path.join(B.BUILD_DIR, o), objects / o)
+    san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+           "-Xarch_host", "-fno-sanitize-recover=all"]
+    r = subprocess.run([B.hipcc(), *B.flags_for("paged_api.hip"), *san, "-c", os.path.join(B.CSRC, "paged_api.hip"), "-o",
+                        str(objects / "paged_api.o")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    monkeypatch.setattr(B, "BUILD_DIR", str(objects))
     other.test_host_code_under_asan_and_ubsan(tmp_path)
 
 
