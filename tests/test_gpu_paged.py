@@ -424,6 +424,18 @@ def test_attention_long_lines(dtype):
     check(db, st, np.ones(st.Nt), q, k, v)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_count", [[1], [1] * 2, [1] * 3, [1] * 5, [6], [6] * 2, [6] * 3, [40, 0, 5, 1], [40] * 3])
+def test_attention_of_long_tasks(q_count, dtype):
+    """One, two and more tasks of many pieces on either line, prompts of several row groups beside prompts of one."""
+    r = np.random.default_rng(sum(q_count))
+    ctx = 1400 + 37 * np.arange(len(q_count))
+    seg = r.integers(0, 50, size=sum(q_count))
+    seg[-1] = 900
+    db, st, q, k, v = filled(q_count, ctx, seg, (8, 2), 64, dtype, 32, seed=len(q_count))
+    check(db, st, np.arange(st.Nt) != 3, q, k, v)
+
+
 def test_attention_many_prompts():
     """More prompts than a window of the plan's scans; most contexts on the wave line, some empty."""
     b = 1100
