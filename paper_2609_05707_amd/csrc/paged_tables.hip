@@ -535,7 +535,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   __syncthreads();
 
   // tiles of the two lines
-  int64_t t1 = 0, t2 = 0, T1, T2, c1 = 0, none = 0, C1, zero;
+  int64_t t1 = 0, t2 = 0, T1, T2, c1 = 0, none = 0, C1 = 0, zero;
   if (!bad) {
     for (int b = tid; b < B; b += threads) {
       const int n = rank(start(b + 1)) - rank(start(b)), tiles = tiles_of(len(b));
@@ -551,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
     for (int k = tid; k < nact; k += threads) t2 += tiles_of(len(B + list(k)));
   }
   scan(t1, t2, T1, T2);
-  scan(c1, none, C1, zero);
+  if (T1 > 0) scan(c1, none, C1, zero);
   // workgroups to the lines by their shares of the work, runs of
   // p.wave_shortest tiles at least on the wave line.  Bound by the stream (bf16) a
   // tile costs a workgroup the same on either line (twice as much on the block
@@ -585,6 +585,10 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
           per = (n + groups - 1) / groups;           // (and ceil(n / per) is groups again)
         }
       }
+    }
+    if (T1 == 0) {                                   // no block line
+      if (b < B) prompt(b) = make_int4(kind, 0, 0, r0);
+      continue;
     }
     const int tiles = tiles_of(tokens);
     int64_t task0 = groups, at0 = static_cast<int64_t>(groups) * (tiles + kSetup), ntask, ntile;
