@@ -22,7 +22,7 @@ namespace {
 
 // Up to so many rows a workgroup takes one row, above them eight.  32 + 8 heads x
 // 128, bf16: 1500 rows without queries 11.2 us by one and 9.1 by eight, with them
-// 14.4 and 18.4, 3000 rows 23.6 and 21.5.
+// 14.4 and 18.4, 3000 rows 23.6 and 20.8.
 constexpr int kStepRows = 1024, kStepRowsWithQueries = 2048;
 
 template <typename T> struct Vec16 { static constexpr int N = 16 / static_cast<int>(sizeof(T)); typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
@@ -109,8 +109,8 @@ __global__ __launch_bounds__(1024) void append_row_kernel(PagedAppendParams p) {
 }
 
 // Eight rows a workgroup.  Waves 0 and 1 turn keys, 2 and 3 carry the values,
-// then all turn the queries: lane (row, 8 pairs) evaluates its angles once for
-// all heads.  Values: eight rows in consecutive slots of one 8-token block are
+// then all turn the queries: lane (row, 8 pairs) holds its angles' cos and sin for
+// all heads, evaluated once for the workgroup.  Values: eight rows in consecutive slots of one 8-token block are
 // transposed in registers into pieces of a dim's eight tokens, put in order in
 // LDS and written as whole lines, by the workgroup that holds the first of them,
 // so that a fill whose rows do not start on a multiple of eight writes whole
@@ -119,7 +119,8 @@ __global__ __launch_bounds__(1024) void append_row_kernel(PagedAppendParams p) {
 // The inputs and the values' lines go with the non-temporal hint, the keys without:
 // 30.7k tokens of 8 heads x 128 (252 MB moved), bf16: 67 us with values in 16-byte
 // pieces (129 with the hint, which then writes parts of lines), 63.5 by whole
-// lines, 55.4 (4.5 TB/s) with the hint on them, 57.9 with it on the keys as well.
+// lines, 55.4 with the hint on them, 57.9 with it on the keys as well, 54.2 (4.6 TB/s)
+// with angles evaluated once a workgroup and not once a wave.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   typedef typename Vec8<T>::type vec_t;
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   // slots of rows r0 - 7 .. r0 + 14: whether a block is whole takes its rows' all
   __shared__ int near[24];
   __shared__ vec_t turn_v[2][64 * 8];
+  __shared__ __attribute__((aligned(16))) float2 rot[8][half];
   if (threadIdx.x < 22) {
     const int r = r0 - 7 + static_cast<int>(threadIdx.x);
     int slot = r >= 0 && r < p.num_rows ? p.slot_map[r] : -1;
@@ -140,17 +142,42 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   }
   const int t = lane / P % 8, j0 = (lane % P) * 8, hs = lane / (8 * P);
   const int row = min(r0 + t, p.num_rows - 1);
-  const int pos = p.positions[row];
-  float cs[8], sn[8];
-  if (wave < 2 || p.q) {
+  const T* ksrc = static_cast<const T*>(p.k) + row * p.k_stride + j0;
+  const T* qsrc = static_cast<const T*>(p.q) + row * p.q_stride + j0;
+  struct Halves { vec_t lo, hi; } kf, qf;
+  auto load = [&](const T* src) {
+    return Halves{__builtin_nontemporal_load(reinterpret_cast<const vec_t*>(src)),
+                  __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(src + half))};
+  };
+  // fp32: the first head of each goes out before the slots are known (12k rows of 6 +
+  // 2 heads x 64 23.4 -> 20.2 us; bf16, whose registers then allow fewer waves,
+  // 30.7k tokens 54.2 -> 58.2)
+  constexpr bool EARLY = sizeof(T) == 4;
+  const int h0 = wave * HPW + hs;
+  if constexpr (EARLY) {
+    if (wave < 2 && h0 < p.Hkv) kf = load(ksrc + h0 * D);
+    if (p.q && h0 < p.Hq) qf = load(qsrc + h0 * D);
+  }
+  {
+    const int mine = threadIdx.x / 32, pos = p.positions[min(r0 + mine, p.num_rows - 1)];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) rope_cos_sin(pos, p.inv_freq[j0 + u], cs[u], sn[u]);
+    for (int j = threadIdx.x % 32; j < half; j += 32) {
+      float c, s;
+      rope_cos_sin(pos, p.inv_freq[j], c, s);
+      rot[mine][j] = make_float2(c, s);
+    }
   }
   __syncthreads();
+  float cs[8], sn[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const float2 x = rot[t][j0 + u];
+    cs[u] = x.x;
+    sn[u] = x.y;
+  }
   const int slot = r0 + t < p.num_rows ? near[7 + t] : -1;
-  auto turn = [&](const T* src, T* dst) {
-    const vec_t lo = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(src));
-    const vec_t hi = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(src + half));
+  auto turn = [&](const Halves& f, T* dst) {
+    const vec_t lo = f.lo, hi = f.hi;
     vec_t x, y;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -164,11 +191,11 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
   };
   if (wave < 2) {
     if (slot >= 0) {
-      const T* src = static_cast<const T*>(p.k) + row * p.k_stride + j0;
       T* dst = static_cast<T*>(p.k_pages) + key_at(p, slot, 0) + j0;
       const int64_t head = static_cast<int64_t>(D) << p.page_shift;
+      if (EARLY && h0 < p.Hkv) turn(kf, dst + h0 * head);
 #pragma unroll 4
-      for (int g = wave * HPW + hs; g < p.Hkv; g += 2 * HPW) turn(src + g * D, dst + g * head);
+      for (int g = h0 + (EARLY ? 2 * HPW : 0); g < p.Hkv; g += 2 * HPW) turn(load(ksrc + g * D), dst + g * head);
     }
   } else {
     const T* v = static_cast<const T*>(p.v);
@@ -218,10 +245,10 @@ __global__ __launch_bounds__(256) void append_rows_kernel(PagedAppendParams p) {
     }
   }
   if (p.q && slot >= 0) {
-    const T* src = static_cast<const T*>(p.q) + row * p.q_stride + j0;
     T* dst = static_cast<T*>(p.q_rot) + static_cast<int64_t>(row) * p.Hq * D + j0;
+    if (EARLY && h0 < p.Hq) turn(qf, dst + h0 * D);
 #pragma unroll 4
-    for (int h = wave * HPW + hs; h < p.Hq; h += 4 * HPW) turn(src + h * D, dst + h * D);
+    for (int h = h0 + (EARLY ? 4 * HPW : 0); h < p.Hq; h += 4 * HPW) turn(load(qsrc + h * D), dst + h * D);
   }
 }
 
