@@ -403,6 +403,8 @@ static_assert(kShortest > kSetup, "a piece may not lie between two tasks' tiles"
 
 // a / b for 0 <= a < 2^52, 0 < b.  The double nearest a / b is on the quotient's side
 // of the next integer: a / b lies 1 / b below it at least, which is 1 / a of it.
+// (A line has fewer than 2^47 places.  The lines' shares may come from more, and are
+// then near enough.)
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return static_cast<int64_t>(static_cast<double>(a) / static_cast<double>(b));
 }
