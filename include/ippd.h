@@ -440,8 +440,9 @@ typedef struct ippd_pages {
  * its tokens: the k-th page taken is the k-th from the top of the stack, and a
  * call that takes back what the call before it added restores the stack.
  * Lengths, offsets or counts that break the rules set IPPD_FLAG_BAD_LAYOUT and
- * the whole call moves nothing (served 0, slots -1).  A page id from the stack
- * or a table that lies outside the pool sets the flag, and the rows in it get -1.
+ * the whole call moves nothing (served 0, slots -1).  A page id outside the pool
+ * that the call moves or writes rows in sets the flag too: the rows in it get -1,
+ * and one that a table gives back goes to the stack as it is.
  * num_rows <= IPPD_PAGED_MAX_ROWS.  slot_map, positions and served overlap none of
  * the batch's arrays or each other.
  */

@@ -282,7 +282,11 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(ReserveParams p) {
                  [&](int k, int w) {
                    return p.block_table[static_cast<int64_t>(s0 + w) * p.table_pages + from[w] + (k - first[w])];
                  },
-                 [&](int k, int, int page) { p.free_pages[f1 - 1 - (carry + k)] = page; });
+                 [&](int k, int, int page) {
+                   // (an id outside the pool goes back too: the stack's count holds, and its next taker gets no slot)
+                   if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.num_pages)) raise_flag(p.err_flag, kFlagBadLayout);
+                   p.free_pages[f1 - 1 - (carry + k)] = page;
+                 });
       carry += total;
     }
   }
