@@ -434,8 +434,8 @@ typedef struct ippd_pages {
  *   positions [num_rows]  its virtual position, by the lengths after the call, or -1;
  *   served [B + Nt]       tokens added to (or, negative, taken from) each sequence.
  * A sequence is served whole or not at all: not if its row of the table is full
- * (IPPD_FLAG_SEGMENT_FULL), nor if the pages needed by the sequences up to it
- * outnumber the free ones (IPPD_FLAG_PAGES_EXHAUSTED).
+ * (IPPD_FLAG_SEGMENT_FULL), nor if it needs a page and the pages needed by the
+ * sequences up to it outnumber the free ones (IPPD_FLAG_PAGES_EXHAUSTED).
  * Pages are taken and given back in the order of sequences and, within one, of
  * its tokens: the k-th page taken is the k-th from the top of the stack, and a
  * call that takes back what the call before it added restores the stack.
