@@ -26,7 +26,8 @@ namespace {
 constexpr int kStepRows = 1024, kStepRowsWithQueries = 2048;
 
 template <typename T> struct Vec16 { static constexpr int N = 16 / static_cast<int>(sizeof(T)); typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
-template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8))); };
+// (tensors and pages are promised at 16 bytes, eight floats by themselves would ask for 32)
+template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8), aligned(16))); };
 
 // Element of the slot's key row, and of column 0 of its value block, for kv head g.
 __device__ __forceinline__ int64_t key_at(const PagedAppendParams& p, int slot, int g) {

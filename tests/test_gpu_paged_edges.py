@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests import paged_reference as R
-from tests.test_gpu_paged import dev32, make, reserve, tables_of
+from tests.test_gpu_paged import BASE, dev32, half_step, make, put, reserve, tables_of
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,49 @@ def test_bad_page_in_a_part_that_stays_is_not_met_by_a_shrink():
     st.table[0, 1] = 8
     db.block_table[0, 1] = 8
     reserve(db, st, [-30], [0, 0], 0)
+
+
+# ----------------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,with_q", [(37, True), (1030, False), (2061, True)])
+def test_append_of_tensors_at_16_bytes(rows, with_q, d, dtype):
+    """Views, pages and results that lie at 16 mod 32 bytes, rows an odd multiple of 16 bytes apart."""
+    hq, hkv, page = 6, 2, 32
+    bf = dtype == "bf16"
+    td, unit = (torch.bfloat16, 8) if bf else (torch.float32, 4)        # elements of 16 bytes
+    r = np.random.default_rng(rows + d)
+    num_pages = -(-(rows + 3) // page) + 1
+
+    def off(*shape, fill=7.0):
+        flat = torch.full((int(np.prod(shape)) + unit,), fill, dtype=td, device="cuda")
+        t = flat[unit:].view(*shape)
+        assert t.data_ptr() % 32 == 16
+        return t
+
+    kp, vp = off(num_pages, hkv, page, d), off(num_pages, hkv, page // 8, d, 8)
+    db, _ = make([1], (hq, hkv), d, dtype, page, num_pages, num_pages, k_pages=[kp], v_pages=[vp])
+    tok = 3 + np.arange(rows)
+    order = r.permutation(num_pages)
+    slots = order[tok // page] * page + tok % page
+    pos = r.integers(0, 100000, size=rows)
+    heads = (hq, hkv, hkv)
+    x, host = [], []
+    for h in heads:
+        wide = off(rows, h * d + unit)
+        assert wide.stride(0) // unit % 2 == 1
+        wide.copy_(torch.from_numpy(r.standard_normal(tuple(wide.shape)).astype(np.float32)))
+        x.append(wide[:, :h * d])
+        host.append(x[-1].double().cpu().numpy().reshape(rows, h, d))
+    q_rot = off(rows, hq, d)
+    db.append(0, dev32(slots), dev32(pos), x[1], x[2], x[0] if with_q else None, q_rot if with_q else None)
+    assert db.err_flag() == 0
+    want_k, want_v = np.full(kp.shape, 7.0), np.full(vp.shape, 7.0)
+    put(want_k, want_v, slots, R.rotate(host[1], pos, BASE), host[2], page)
+    assert np.array_equal(vp.double().cpu().numpy(), want_v)
+    size = max(np.abs(h).max() for h in host)
+    err = np.abs(kp.double().cpu().numpy() - want_k)
+    assert (err <= half_step(want_k, bf) + 2 * size * (2e-7 + 2 * R.U32)).all()
+    want = R.rotate(host[0], pos, BASE) if with_q else np.full((rows, hq, d), 7.0)
+    err = np.abs(q_rot.double().cpu().numpy() - want)
+    assert (err <= half_step(want, bf) + 2 * size * (2e-7 + 2 * R.U32)).all()
