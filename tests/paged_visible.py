@@ -112,3 +112,23 @@ def lines():
         seg = r.integers(0, 50, size=sum(q_count))
         seg[-1] = 900
         yield f"long tasks {q_count}", q_count, 1400 + 37 * np.arange(len(q_count)), seg
+
+
+# Pieces of the block line longer than twice the LDS ring's stages: 32 kv heads leave 16 workgroups a head (8 with eight
+# waves), and the piece per workgroup grows with the lengths.  (type, head_dim, max_questions, waves, stages); G = 2, so
+# max_questions alone chooses the waves and whether one or two 16-row blocks are a wave's.
+KINDS = [("bf16", 64, 32, 4, 9), ("bf16", 64, 64, 4, 9), ("bf16", 64, 130, 8, 9),
+         ("bf16", 128, 32, 4, 5), ("bf16", 128, 64, 4, 5), ("bf16", 128, 130, 8, 9),
+         ("f32", 64, 32, 4, 5), ("f32", 128, 64, 8, 4)]
+
+
+def runs(dtype, max_questions, waves, stages):
+    """Questions, contexts and segments of a kind: an odd number of tokens in each last tile, few segments."""
+    q_count = {32: [20, 9, 32], 64: [40, 9, 64], 130: [70, 9, 130]}[max_questions]
+    if waves == 4:
+        tiles = [int(3 * stages * x) for x in (5.5, 0.3, 8.6)]
+    else:                                                      # (130 questions are two row groups, each over all its tiles)
+        tiles = [int(4 * stages * x) for x in (1.5, 0.2, 2.5 if dtype == "bf16" else 4.9)]
+    ctx = np.array([32 * tiles[0] - 13, 32 * tiles[1] - 31, 32 * tiles[2] - 1])
+    seg = np.array([(7 * i) % 70 if i % 12 == 3 else 0 for i in range(sum(q_count))])
+    return q_count, ctx, seg

@@ -1,5 +1,5 @@
 """GPU: the paged attention where a wrong tile shows in the outputs (tests/paged_visible.py), at lengths that cut the
-lines into many pieces."""
+lines into many pieces and in pieces that pass the LDS ring more than twice."""
 import numpy as np
 import pytest
 import torch
@@ -45,6 +45,26 @@ def check(db, st, active, q, k, v):
     assert err.max() <= 1, err.max()
 
 
+def cut(db):
+    """(waves, tiles a workgroup takes of a task of the block line, those of tasks that a piece goes on into), checked
+    against the tasks' tiles."""
+    w = db.plan_buf.view(torch.int32).cpu().numpy()
+    groups, n1, tasks, waves = int(w[3]), int(w[6]), int(w[10]), int(w[11])
+    task1 = 64 + 12 * groups * (1 + waves)
+    task = w[task1:task1 + 8 * tasks].reshape(-1, 8)
+    first, later, seen = [], [], np.zeros(tasks, dtype=int)
+    for b in range(n1):
+        i, _, n = w[64 + 12 * b:64 + 12 * b + 3]
+        first.append(int(n))
+        seen[i] += n
+        while i + 1 < tasks and task[i + 1, 5] == b:
+            i += 1
+            later.append(int(task[i, 7]))
+            seen[i] += task[i, 7]
+    assert np.array_equal(seen, task[:, 6])
+    return waves, first, later
+
+
 LINES = list(V.lines())
 
 
@@ -55,3 +75,17 @@ def test_every_tile_of_long_lines(case, d, page, dtype):
     _, q_count, ctx, seg = LINES[case]
     db, st, q, k, v = filled(q_count, ctx, seg, (8, 2), d, dtype, page, case)
     check(db, st, np.arange(st.Nt) != 3, q, k, v)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dtype,d,most,waves,stages", V.KINDS)
+def test_pieces_longer_than_the_ring(dtype, d, most, waves, stages, page):
+    """Odd and even runs of more than twice the ring's stages, and runs of more than the ring in a piece's next task."""
+    q_count, ctx, seg = V.runs(dtype, most, waves, stages)
+    db, st, q, k, v = filled(q_count, ctx, seg, (64, 32), d, dtype, page, most + d, max_questions=most)
+    check(db, st, np.arange(st.Nt) != 7, q, k, v)
+    got, first, later = cut(db)
+    assert got == waves
+    long = [n for n in first if n > 2 * stages]
+    assert {n % 2 for n in long} == {0, 1}, first
+    assert max(later) > stages, later

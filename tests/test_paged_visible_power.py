@@ -7,6 +7,7 @@ from tests import paged_reference as R
 from tests import paged_visible as V
 
 LENGTHS = [(name, q, ctx, seg, dt, d) for name, q, ctx, seg in V.lines() for dt, d in (("bf16", 128), ("bf16", 64), ("f32", 64))]
+LENGTHS += [(f"runs {dt} {d} {most}", *V.runs(dt, most, waves, stages), dt, d) for dt, d, most, waves, stages in V.KINDS]
 
 
 def plant(mistake, st, seq, tile, k, v):
