@@ -89,3 +89,28 @@ def test_pieces_longer_than_the_ring(dtype, d, most, waves, stages, page):
     long = [n for n in first if n > 2 * stages]
     assert {n % 2 for n in long} == {0, 1}, first
     assert max(later) > stages, later
+
+
+@pytest.mark.parametrize("d,dtype,most", [(128, "bf16", 8), (64, "f32", 8), (128, "bf16", 40)])
+@pytest.mark.parametrize("page", [256, 16])
+def test_both_lines_in_pages_beyond_32_bits(page, d, dtype, most):
+    """A context with more than 16 rows (the block line), one with fewer and the segments (the wave line), in a small
+    pool and in pages of a large one that lie more than 2^32 elements behind its first, the rest of it NaN: bit for bit."""
+    q_count, ctx, seg = [8, 2], [1300, 500], [40, 3, 17, 300, 0, 9, 60, 1, 33, 5]
+    heads = (32, 8)
+    db, st, q, k, v = filled(q_count, ctx, seg, heads, d, dtype, page, page + d, max_questions=most)
+    check(db, st, np.ones(st.Nt), q, k, v)
+    out, ls = run(db, q)
+    offset = 2 ** 32 // (heads[1] * page * d) + 3
+    large = PagedBatch(q_count, *heads, d, dtype, page, offset + st.num_pages, st.table_pages, rope_base=BASE,
+                       max_questions=most)
+    for big, small in ((large.k_pages[0], db.k_pages[0]), (large.v_pages[0], db.v_pages[0])):
+        big.fill_(float("nan"))
+        big[offset:] = small
+        assert big[offset].data_ptr() - big.data_ptr() > 2 ** 32 * big.element_size()
+    large.block_table.copy_(db.block_table + offset)
+    large.seq_len.copy_(db.seq_len)
+    got, gl = run(large, q)
+    assert large.err_flag() == 0
+    assert torch.equal(got, out) and torch.equal(gl, ls)
+    assert cut(large)[1] and int(large.plan_buf.view(torch.int32)[7]) > 0        # pieces of both lines
