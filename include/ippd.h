@@ -488,7 +488,7 @@ ippd_status_t ippd_paged_plan(const ippd_paged_batch_t *batch, void *plan, size_
  * all of its active questions.  q_rot and out [Nt][Hq][D] are of the batch
  * dtype (the output feeds a projection of that type; sums and softmax
  * statistics are fp32), lse [Nt][Hq] float32 or NULL.  A question without any
- * key gets zeros and lse -inf.  Rows of inactive questions are not written, nor
+ * key, or whose scores are all -inf, gets zeros and lse -inf.  Rows of inactive questions are not written, nor
  * those of a question that a page id outside the pool is met for
  * (IPPD_FLAG_BAD_LAYOUT).  A buffer that holds no plan of this batch's sizes
  * sets the same flag and nothing is written.
