@@ -486,8 +486,11 @@ ippd_status_t ippd_paged_plan(const ippd_paged_batch_t *batch, void *plan, size_
  * over the keys of its prompt's context and of its own segment (the step's own
  * token among them, if it was appended).  A context's pages are read once for
  * all of its active questions.  q_rot and out [Nt][Hq][D] are of the batch
- * dtype (the output feeds a projection of that type; sums and softmax
- * statistics are fp32), lse [Nt][Hq] float32 or NULL.  A question without any
+ * dtype (the output feeds a projection of that type), lse [Nt][Hq] float32 or
+ * NULL.  Scores, softmax statistics and sums are fp32; for the product with the
+ * values of a bf16 cache each weight is rounded to bf16 (by 2^-8 of it at most), so
+ * that an element of out is off by up to 2^-8 of the mean of |V| under the
+ * softmax, and by its own rounding.  A question without any
  * key, or whose scores are all -inf, gets zeros and lse -inf.  Rows of inactive questions are not written, nor
  * those of a question that a page id outside the pool is met for
  * (IPPD_FLAG_BAD_LAYOUT).  A buffer that holds no plan of this batch's sizes

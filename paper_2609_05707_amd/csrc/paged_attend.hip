@@ -55,7 +55,12 @@ __device__ __forceinline__ void clear(State<D>& st) {
 
 // Folds a tile's scores (lane (lg, lr): tokens 8 lg + 4 kb + v of row lr) into
 // the state and returns the weights as the value product's operand, rounded to
-// the cache's type (bf16: half a step, 2^-9, each; the sum keeps 32 bits).  The
+// the cache's type, since a matrix instruction takes both operands in one (bf16:
+// off by 2^-8 of each at most; the sum keeps 32 bits).  A norm-wise error of
+// 0.0023 in the outputs where their own rounding is 0.0017; a second product, with
+// what the rounding left, ends at 0.0017 too, for 179 -> 226 us at 32768 tokens x
+// 64 questions (three layers), 313 -> 325 on 32 ragged prompts (two), 118 -> 124 at
+// 4096 x 16 (eight), and makes NaN of an infinite value (times 0).  The
 // offset m moves only when a score exceeds it by 2^8 in the exponent.
 template <typename T, int D>
 __device__ __forceinline__ typename Mfma<T>::Frag fold(const f32x4_t (&sc)[2], State<D>& st, float c) {
