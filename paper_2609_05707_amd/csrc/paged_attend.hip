@@ -354,9 +354,10 @@ __device__ __forceinline__ void stream(const PagedAttendParams& p, unsigned char
     rest(now, next);
   };
   int t = 0;
-  for (; put + 1 <= end; t += 2) {
+  while (put + 1 <= end) {                           // (a full step moves put)
     full(sa, sb);
     full(sb, sa);
+    t += 2;
   }
   for (; t + 2 <= last; t += 2) {
     drain(t, sa, sb);
