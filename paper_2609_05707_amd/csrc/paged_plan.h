@@ -21,7 +21,8 @@ inline ippd_status_t check_paged(const ippd_paged_batch_t* bt) {
     return IPPD_ERR_SHAPE;
   if (bt->num_q_heads % bt->num_kv_heads != 0) return IPPD_ERR_SHAPE;
   if (bt->num_q_heads / bt->num_kv_heads > kMaxGroup || bt->num_q_heads > 1024) return IPPD_ERR_SHAPE;
-  if (static_cast<int64_t>(bt->num_questions) * bt->num_kv_heads > (1 << 23)) return IPPD_ERR_SHAPE;   // the join's grid
+  // partial states of 2 x G rows a question and kv head: at 2^23, D = 128, over 8 GB for each query head of a kv head
+  if (static_cast<int64_t>(bt->num_questions) * bt->num_kv_heads > (1 << 23)) return IPPD_ERR_SHAPE;
   if (bt->head_dim != 64 && bt->head_dim != 128) return IPPD_ERR_SHAPE;
   const int p = bt->page_tokens;
   if (p != 16 && p != 32 && p != 64 && p != 128 && p != 256) return IPPD_ERR_SHAPE;
@@ -53,9 +54,10 @@ inline PagedShape paged_shape(const ippd_paged_batch_t* bt) {
   s.page_shift = page_shift_of(bt->page_tokens);
   const bool bf16 = bt->dtype == IPPD_DTYPE_BF16;
   const int most = bt->max_questions * s.G;
-  // Eight waves, and a compute unit's LDS to themselves, where a context has more
-  // rows than four waves hold (a second row group would stream it again), and for
-  // fp32 at head_dim 128, whose ring leaves no room for a second workgroup.
+  // Eight waves, one workgroup on a compute unit, where a context has more rows than
+  // four waves hold (a second row group would stream it again), and for fp32 at
+  // head_dim 128, whose ring leaves no room for a second workgroup.  (bf16 at head_dim
+  // 64: the nine stages are 72 of a unit's 160 KB.)
   s.waves = (bf16 ? most > 128 : bt->head_dim == 128) ? 8 : 4;
   s.rb = most <= 16 ? 0 : bf16 && most > 64 ? 2 : 1;
   s.by_rows = bf16 ? 0 : 1;

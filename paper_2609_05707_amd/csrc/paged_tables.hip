@@ -138,8 +138,8 @@ __device__ __forceinline__ int last_at_most(const A& a, int n, int x) {
 // that page k falls to: thread t's has the pages ex .. ex + n - 1.  first: ex of
 // each, in LDS (a barrier lies behind it).  Few pages find theirs by a search each;
 // of more a thread takes kPer in a row, and the sequence of a page is the last that
-// marked one up to it.  Some 6k pages of 608 sequences take
-// 7.8 us a call, 1.4 more with a search and a round trip each (6 more with four
+// marked one up to it.  5679 pages of 671 sequences take
+// 7.9 us a call, 1.4 more with a search and a round trip each (6 more with four
 // searches at once: the searches' instructions are what costs).
 constexpr int kPer = 4;
 static_assert(kThreads <= 1 << 16, "a mark has 16 bits");
@@ -563,8 +563,8 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PagedPlanParams p) {
   // tile costs a workgroup the same on either line (twice as much on the block
   // line: 8 prompts of 8192 x 32 248 -> 269 us, three layers; three quarters
   // 235).  Bound by the products (fp32) it costs half as much as it has row
-  // blocks: 64 rows of 128-wide heads 96 us at 4 and 67 at 2, 128 rows 172 at 4
-  // and 230 at 2.
+  // blocks: 8 prompts of 4096 tokens, 8 kv heads x 128, 64 rows 165 us at 4 and 105
+  // at 2, 128 rows 181 at 4 and 201 at 2.
   int n1 = 0, n2 = 0;
   if (T1 > 0) {
     const int64_t most = p.W - (T2 > 0 ? 1 : 0), all = C1 + 2 * T2;

@@ -32,7 +32,9 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 
 class PagedBatch:
     """Prompts with ``q_count`` questions each on one GPU; sequences 0..B-1 are their
-    contexts, B..B+Nt-1 the questions' segments, all empty at first.
+    contexts, B..B+Nt-1 the questions' segments, all empty at first.  ``q_count`` is
+    fixed: a prompt that takes the place of one that ended has at most as many
+    questions, the rest of the place staying inactive and empty.
 
     Tables and pages are made here (every page free, page 0 taken first) unless
     tensors that the caller keeps are given: seq_len int32 [B+Nt], block_table
